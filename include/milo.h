@@ -325,6 +325,155 @@ int milo_block_factors(const uint16_t* const* k, const int32_t* tokens, int32_t 
 int milo_block_svd_sweeps(int32_t* sweeps);
 int milo_block_svd_flops(double* flops);
 
+/* ---------------------------------------------------------------------------
+ * Paged 8-bit cache of the requests' own keys and values.
+ *
+ * A pool of pages that requests of any length share, with lengths, tables and
+ * free pages in device memory, so that a serving step needs no host copy:
+ *   milo_pages_plan    lengths and pages after a step, slots of its new rows
+ *   milo_pages_store   the new rows' keys and values quantised into their slots
+ *   milo_attend_pages  attention of the step's queries over each request's rows
+ *   milo_pages_load    rows back to bf16 (e.g. as the input of milo_block_svd)
+ * All four are asynchronous, allocate nothing, copy nothing from or to the host
+ * and may be captured into a graph; what they need besides their arguments is
+ * in buffers of the caller.  All buffers are device memory of the current
+ * device.  Values that only the device knows (lengths, ids, slots) are checked
+ * there: a value out of range never leads to an access out of range; what it
+ * does instead is said at each function.
+ * ------------------------------------------------------------------------- */
+
+/* A page holds page_tokens consecutive rows (tokens) of one request, all KV
+ * heads, with one fp32 scale per (page, head) for keys and one for values: a
+ * row's value is scale * code.  Slot page * page_tokens + offset names one row.
+ *   n_pages      >= 1, n_pages * page_tokens <= 2^31 - 1
+ *   page_tokens  16, 32, 64 or 128
+ *   n_kv_heads   H_kv >= 1
+ *   head_dim     d, 64 or 128
+ *   format       MILO_KV_INT8   codes -127 .. 127; scale = amax / 127 (fp32,
+ *                               correctly rounded), code = round-half-even(x / scale)
+ *                MILO_KV_E4M3   8-bit floating point (4 exponent bits, 3 fraction
+ *                               bits, bias 7, largest value 448); scale = the smallest
+ *                               power of two with amax <= 448 scale (at least 2^-126),
+ *                               code = x / scale rounded half to even
+ *                (amax: the largest magnitude of the page's rows of that head)
+ *   k_codes      [n_pages][H_kv][page_tokens * d] bytes, 16-byte aligned; in a page
+ *                and head [token/16][dim/16][token%16][dim%16]
+ *   v_codes      the same size, [token/16][dim/64][token%16/4][dim%16][dim%64/16][token%4]
+ *   k_scale, v_scale  [n_pages][H_kv] fp32
+ * Both orders make 16 rows of a head one contiguous run whose pieces are operands
+ * of matrix instructions: keys 16 dims of a token, values 4 tokens of 4 dims that
+ * lie 16 apart. */
+#define MILO_KV_INT8 0
+#define MILO_KV_E4M3 1
+typedef struct milo_pages {
+  int32_t n_pages;
+  int32_t page_tokens;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t format;
+  void* k_codes;
+  void* v_codes;
+  float* k_scale;
+  float* v_scale;
+} milo_pages;
+
+/* Lengths, pages and slots of a step.  Request i holds lens[i] rows in the first
+ * ceil(lens[i] / page_tokens) pages of its row of `table`; delta[i] > 0 appends as
+ * many rows, delta[i] < 0 gives up its last -delta[i] rows (all of them when it
+ * ends).  Pages it needs come from the ring of free pages, pages it no longer
+ * needs go there.
+ *   lens, delta  [n_req], n_req >= 0
+ *   table        [n_req][table_width] page ids, table_width >= 1; new entries are
+ *                written, all others stay (entries past a request's pages mean nothing)
+ *   ring         [n_pages] free page ids, n_pages >= 1: the free ones are ring[(head + k) mod
+ *                n_pages], k < count; pages are taken from the head, request by
+ *                request, and given back behind the last
+ *   ring_state   [2] head and count; ring_state_out [2] those after the step (may be
+ *                the same buffer)
+ *   lens_out     [n_req] lens + delta (may be lens itself)
+ *   starts       [n_req + 1] first packed row of each request's new rows: the running
+ *                sums of max(delta, 0)
+ *   slots        [n_slots] slot of each packed new row; -1 behind the last and for a row
+ *                whose page id is outside [0, n_pages)
+ *   status       [1] 0, or the sum of what stopped the step:
+ *                  1 too few free pages              2 a row of the table is too narrow
+ *                  4 a length or delta below range   8 n_slots below the new rows
+ *                 16 ring_state is not that of a ring, or more pages come back than it holds
+ *                then nothing changes: lens_out = lens, ring_state_out = ring_state,
+ *                table and ring stay, starts are all 0 and slots all -1.
+ *   work         milo_pages_plan_work(n_req) bytes, 16-byte aligned
+ * The step's result does not depend on the order in which the GPU runs it.
+ * Errors: INVALID_ARG (NULL pointer, sizes), UNSUPPORTED (page_tokens, n_pages *
+ * page_tokens or n_req over 2^24), HIP_ERROR. */
+int64_t milo_pages_plan_work(int32_t n_req);
+int milo_pages_plan(const int32_t* lens, const int32_t* delta, int32_t n_req, int32_t page_tokens,
+                    int32_t* table, int32_t table_width, int32_t* ring, int32_t n_pages,
+                    const int32_t* ring_state, int32_t* ring_state_out, int32_t* lens_out,
+                    int32_t* starts, int32_t* slots, int32_t n_slots, int32_t* status, void* work,
+                    void* hip_stream);
+
+/* Quantise n_tok rows of keys and values into their slots.  Row j's keys are
+ * k + j * k_stride (bf16 [H_kv][d], the stride in elements, a multiple of 8;
+ * 16-byte aligned), its values likewise.  slots [n_tok]: row j's slot; a slot
+ * outside [0, n_pages * page_tokens) skips its row.  Rows of one page must follow
+ * one another in the call with ascending slots without gaps, as milo_pages_plan
+ * gives them, and a page appears once (otherwise the codes and scales of the pages
+ * concerned, of no other, are undefined).
+ * Rows of a page before its first new one are held: where a new row needs a larger
+ * scale, their codes c become those of c * old scale under the new one (each time
+ * rounded; INT8: at most half a step of the new scale more per growth; E4M3: exact
+ * but below its smallest normal value).  Scales never shrink but when a page's first
+ * row is written, which starts the page afresh.  Rows behind the last new one stay
+ * as they are.  A page and head that received a value that is not finite holds NaN
+ * (its scale) until it starts afresh.
+ * Errors: INVALID_ARG, UNSUPPORTED, HIP_ERROR. */
+int milo_pages_store(const milo_pages* pages, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                     int64_t v_stride, const int32_t* slots, int32_t n_tok, void* hip_stream);
+
+/* Rows of pages as bf16 (scale * code in fp32, rounded once): row j of k_out / v_out
+ * ([H_kv][d] each, strides in elements, multiples of 8, 16-byte aligned) is the row in
+ * slot slots[j]; zeros for a slot out of range.  Any order, also the same slot twice.
+ * k_out or v_out may be NULL (not read then).  Errors: INVALID_ARG, UNSUPPORTED, HIP_ERROR. */
+int milo_pages_load(const milo_pages* pages, const int32_t* slots, int32_t n_tok, uint16_t* k_out,
+                    int64_t k_stride, uint16_t* v_out, int64_t v_stride, void* hip_stream);
+
+/* Attention of a ragged batch of queries over the requests' pages and, with a
+ * cache, over selected blocks of its compressed context in the same softmax (Eq. 1
+ * over the blocks and the request's own rows, as milo_attend_decode with the dense
+ * tail held in pages).
+ *   cache        compressed context read by every query, or NULL: pages only (then
+ *                block_table is NULL and n_sel 0).  Same H_kv and d as the pages; its
+ *                path, RoPE and format settings apply; block_table / n_sel as for
+ *                milo_attend_decode.  Its workspace is used: order the calls on it.
+ *   page_table   [n_req][table_width], lens [n_req]: request i's rows are the first
+ *                lens[i] of its pages (lengths are cut to [0, table_width * page_tokens];
+ *                a request one of whose pages is outside [0, n_pages) gets NaN)
+ *   q_starts     [n_req + 1] running sums: request i's queries are rows q_starts[i] ..
+ *                q_starts[i+1] - 1 of q (cut to [0, n_tok]); NULL: query i is request
+ *                i's only one (n_tok == n_req)
+ *   q            bf16, row j at q + j * q_stride ([H_q][d]; stride in elements, a multiple
+ *                of 8; 16-byte aligned); n_tok >= 0 rows
+ *   n_q_heads    H_q, a multiple of H_kv, at most 16 query heads per KV head
+ *   causal       1: a request's queries are its last rows: query j of m sees the first
+ *                lens - m + j + 1 rows.  0: every query sees all rows (cross attention)
+ *   scale        finite
+ *   out          [n_tok][H_q][d], fp32 (out_format MILO_OUT_F32) or bf16 (MILO_OUT_BF16);
+ *                16-byte aligned.  A query that sees nothing gets zeros.  Rows of no request
+ *                (before q_starts[0], from q_starts[n_req] on) are not written.
+ *   work         milo_attend_pages_work bytes, 256-byte aligned: this call's alone until
+ *                its work has run.
+ * Scores, softmax sums and outputs are accumulated in fp32 from the exact codes; the
+ * weights enter the value product in bf16 (2^-9), in two parts (2^-17) for fp32 output.
+ * Errors: INVALID_ARG, UNSUPPORTED, and with a cache those of milo_attend_decode. */
+#define MILO_OUT_F32 0
+#define MILO_OUT_BF16 1
+int64_t milo_attend_pages_work(int32_t n_tok, int32_t n_q_heads, int32_t head_dim, int with_cache);
+int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_sel,
+                      const milo_pages* pages, const int32_t* page_table, int32_t table_width,
+                      const int32_t* lens, const int32_t* q_starts, int32_t n_req, const uint16_t* q,
+                      int64_t q_stride, int32_t n_tok, int32_t n_q_heads, int32_t causal, float scale,
+                      void* out, int32_t out_format, void* work, void* hip_stream);
+
 /* Release the cache and its device memory (synchronises the device first).
  * NULL is accepted and ignored. */
 void milo_cache_free(milo_cache* cache);

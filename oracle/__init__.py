@@ -45,6 +45,10 @@ rows, softmax over all keys, accumulate weights times P^V rows in rank space,
 up-project through R^V, add the dense tail, normalise.  Both use one global
 maximum per column (two-pass softmax) and sum blocks in table order, tokens
 ascending, then the tail.
+
+`pages_plan`, `pages_store`, `pages_scale`, `pages_codes`, `e4m3_round` and
+`attend_pages` are the paged 8-bit cache of the requests' own rows: its
+bookkeeping request by request, its quantisation and attention over its rows.
 """
 from __future__ import annotations
 
@@ -52,8 +56,9 @@ import math
 
 import numpy as np
 
-__all__ = ["allocate_ranks", "attend_dense", "attend_latent", "attend_prefill", "block_factors", "block_svd",
-           "dequantize_rows_int8", "quantize_rows_int8", "reconstruct", "rope", "spectral_information"]
+__all__ = ["allocate_ranks", "attend_dense", "attend_latent", "attend_pages", "attend_prefill", "block_factors",
+           "block_svd", "dequantize_rows_int8", "e4m3_round", "pages_codes", "pages_plan", "pages_scale", "pages_store",
+           "quantize_rows_int8", "reconstruct", "rope", "spectral_information"]
 
 
 def _mm(a: np.ndarray, b: np.ndarray, ordered: bool) -> np.ndarray:
@@ -403,3 +408,128 @@ def block_factors(k, v, r: int):
     rank-r approximation of K."""
     vr = np.asarray(v, dtype=np.float64)[:, :r]
     return np.asarray(k, dtype=np.float64) @ vr, vr.T.copy()
+
+
+# ---- paged 8-bit cache of the requests' own rows (include/milo.h, milo_pages) ----------------
+
+def e4m3_round(x: np.ndarray) -> np.ndarray:
+    """The nearest value of 4 exponent bits (bias 7) and 3 fraction bits, half to even, |x| <= 448."""
+    x = np.asarray(x, dtype=np.float64)
+    _, e = np.frexp(np.where(x == 0, 1.0, x))         # |x| = m 2^e, 0.5 <= m < 1
+    step = np.exp2(np.maximum(e - 1, -6) - 3.0)        # spacing of the values around x
+    return np.rint(x / step) * step
+
+
+def pages_scale(amax: float, e4m3: bool) -> np.float32:
+    """Scale of a page and head whose largest magnitude is amax; NaN where that is not finite."""
+    if not np.isfinite(amax):
+        return np.float32(np.nan)
+    if not e4m3:
+        return np.float32(amax) / np.float32(127)
+    if amax == 0:
+        return np.float32(0)
+    e = -126
+    while amax > 448.0 * 2.0 ** e:
+        e += 1
+    return np.float32(2.0 ** e)
+
+
+def pages_codes(x, s, e4m3: bool) -> np.ndarray:
+    """Code values of x under scale s."""
+    x = np.asarray(x, dtype=np.float32)
+    if not s > 0:
+        return np.zeros(x.shape)
+    if e4m3:
+        return e4m3_round(x.astype(np.float64) / float(s))
+    return np.clip(np.rint(x / np.float32(s)), -127, 127).astype(np.float64)   # fp32 division, as defined
+
+
+def pages_store(rows, scales, page_tokens: int, x, slots, e4m3: bool) -> None:
+    """Append x [n][H][d] into a pool kept as code values rows [n_pages][P][H][d] and float32
+    scales [n_pages][H], both updated: the rows of each page and head in one go."""
+    P = page_tokens
+    j, n = 0, len(slots)
+    while j < n:
+        if not 0 <= slots[j] < rows.shape[0] * P:
+            j += 1
+            continue
+        page, off = divmod(int(slots[j]), P)
+        m = 1
+        while j + m < n and off + m < P and slots[j + m] == slots[j] + m:
+            m += 1
+        for h in range(rows.shape[2]):
+            new = x[j:j + m, h]
+            s, was = pages_scale(np.abs(new).max() if np.all(np.isfinite(new)) else np.nan, e4m3), scales[page, h]
+            if off > 0:
+                s = np.float32(np.nan) if np.isnan(s) or np.isnan(was) else max(s, was)
+                if s > was:
+                    rows[page, :off, h] = pages_codes(rows[page, :off, h].astype(np.float32) * was, s, e4m3)
+            rows[page, off:off + m, h] = pages_codes(new, s, e4m3)
+            scales[page, h] = s
+        j += m
+
+
+def pages_plan(lens, delta, page_tokens: int, table, ring, head: int, count: int, n_slots: int):
+    """A step's bookkeeping, request by request.  Returns (status, lens, starts, slots, table, ring,
+    (head, count)); table and ring are copies."""
+    P, n_pages, width = page_tokens, len(ring), table.shape[1]
+    lens, delta = [int(v) for v in lens], [int(v) for v in delta]
+    table, ring = table.copy(), ring.copy()
+    pages = lambda n: -(-n // P)  # noqa: E731
+    status = 0
+    good = []
+    for n, a in zip(lens, delta):
+        bad = 4 if n < 0 or n + a < 0 else 2 if max(n, n + a) > width * P else 0
+        status |= bad
+        good.append(not bad)
+    taken = sum(max(pages(n + a) - pages(n), 0) for n, a, g in zip(lens, delta, good) if g)
+    given = sum(max(pages(n) - pages(n + a), 0) for n, a, g in zip(lens, delta, good) if g)
+    rows = sum(max(a, 0) for a, g in zip(delta, good) if g)
+    if not (0 <= head < n_pages and 0 <= count <= n_pages and count + given <= n_pages):
+        status |= 16
+    elif taken > count:
+        status |= 1
+    if rows > n_slots:
+        status |= 8
+    slots = np.full(n_slots, -1, dtype=np.int64)
+    if status:
+        return status, lens, [0] * (len(lens) + 1), slots, table, ring, (head, count)
+    starts, out, tail = [0], [], head + count
+    old = table.copy()
+    for i, (n, a) in enumerate(zip(lens, delta)):
+        for p in range(pages(n), pages(n + a)):
+            table[i, p] = ring[head % n_pages]
+            head, count = head + 1, count - 1
+        for r in range(n, n + a):
+            if 0 <= table[i, r // P] < n_pages:              # an id of no page: no slot
+                slots[starts[-1] + r - n] = table[i, r // P] * P + r % P
+        starts.append(starts[-1] + max(a, 0))
+        out.append(n + a)
+    for i, (n, a) in enumerate(zip(lens, delta)):
+        for p in range(pages(n + a), pages(n)):
+            ring[tail % n_pages] = old[i, p]
+            tail, count = tail + 1, count + 1
+    return 0, out, starts, slots, table, ring, (head % n_pages, count)
+
+
+def attend_pages(keys, values, q, scale: float, causal: bool):
+    """One request's queries q [m][H_q][d] over its rows keys / values [n][H_kv][d] in fp64; query j
+    sees the first n - m + j + 1 rows when causal.  Returns (out, size, reach): size = the same
+    average of |values|, reach [m][H_q] = the largest sum |q_c k_c| scale of a score (both for
+    error bounds).  A query that sees nothing gets zeros."""
+    n, m, G = keys.shape[0], q.shape[0], q.shape[1] // keys.shape[1]
+    out, size = np.zeros(q.shape), np.zeros(q.shape)
+    reach = np.zeros(q.shape[:2])
+    for h in range(q.shape[1]):
+        K, V = keys[:, h // G], values[:, h // G]
+        s_all = (q[:, h] @ K.T) * scale
+        r_all = (np.abs(q[:, h]) @ np.abs(K).T) * abs(scale)
+        for j in range(m):
+            c = max(0, n - m + j + 1) if causal else n
+            if c == 0:
+                continue
+            w = np.exp(s_all[j, :c] - s_all[j, :c].max())
+            out[j, h] = w @ V[:c] / w.sum()
+            size[j, h] = w @ np.abs(V[:c]) / w.sum()
+            reach[j, h] = r_all[j, :c].max()
+    return out, size, reach

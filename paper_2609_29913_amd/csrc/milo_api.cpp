@@ -625,7 +625,7 @@ namespace milo {
 int attend_call(milo_cache* c, PlanState& ps, Workspace& ws, const int32_t* block_table, int32_t n_sel, int32_t n_q,
                 int32_t n_q_heads, const uint16_t* q, const uint16_t* tail_k, const uint16_t* tail_v,
                 const int32_t* tail_len, int32_t tail_base, int32_t tail_cap, int64_t tail_stride, float scale,
-                float* out, void* hip_stream) {
+                float* out, void* hip_stream, float2* ml_out) {
   // ---- validation (host only, nothing queued yet) ----
   if (!c) return fail(MILO_ERR_INVALID_ARG, "cache is NULL");
   if (n_sel < 0) return fail(MILO_ERR_INVALID_ARG, "n_sel must be >= 0");
@@ -914,6 +914,7 @@ int attend_call(milo_cache* c, PlanState& ps, Workspace& ws, const int32_t* bloc
   ma.part_o = part_o;
   ma.part_ml = part_ml;
   ma.out = out;
+  ma.ml_out = ml_out;
   ma.slot_count = reinterpret_cast<const int32_t*>(ps.plan_d + ps.count_off);
   ma.H_q = n_q_heads;
   ma.G = G;
@@ -995,6 +996,18 @@ int attend_call(milo_cache* c, PlanState& ps, Workspace& ws, const int32_t* bloc
     if (n_ev == 6) g_timing.recon_recorded.insert(g_timing.recon_recorded.end(), ev + 4, ev + 6);
   }
   return MILO_OK;
+}
+
+int attend_context(milo_cache* c, const int32_t* block_table, int32_t n_sel, int32_t n_q, int32_t n_q_heads,
+                   const uint16_t* q, float scale, float* out, float2* ml_out, void* hip_stream) {
+  CacheWorkspace ws(c);
+  return attend_call(c, c->plan, ws, block_table, n_sel, n_q, n_q_heads, q, nullptr, nullptr, nullptr, -1, 0, 0, scale,
+                     out, hip_stream, ml_out);
+}
+
+void cache_heads(const milo_cache* c, int* n_kv, int* d) {
+  *n_kv = c->n_kv;
+  *d = c->d;
 }
 
 }  // namespace milo

@@ -70,6 +70,13 @@ class Workspace {
 int attend_call(milo_cache* c, PlanState& ps, Workspace& ws, const int32_t* block_table, int32_t n_sel, int32_t n_q,
                 int32_t n_q_heads, const uint16_t* q, const uint16_t* tail_k, const uint16_t* tail_v,
                 const int32_t* tail_len, int32_t tail_base, int32_t tail_cap, int64_t tail_stride, float scale,
-                float* out, void* hip_stream);
+                float* out, void* hip_stream, float2* ml_out = nullptr);
+
+// Attention of n_q queries over the selected blocks alone, through the cache's own
+// workspace: out fp32 [n_q][H_q][d] and per column its maximum (log2 units) and sum,
+// for a caller that merges it with other keys.
+int attend_context(milo_cache* c, const int32_t* block_table, int32_t n_sel, int32_t n_q, int32_t n_q_heads,
+                   const uint16_t* q, float scale, float* out, float2* ml_out, void* hip_stream);
+void cache_heads(const milo_cache* c, int* n_kv, int* d);
 
 }  // namespace milo

@@ -514,6 +514,7 @@ struct MergeArgs {
   int H_q, G, n_block_slots, n_slots;
   TileGeom tiles;
   TailLens tl;
+  float2* ml_out;             // [n_q][H_q] maximum (log2 units) and sum of a column (NULL: not wanted)
 };
 
 struct PackArgs {

@@ -1451,6 +1451,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(MergeArgs a) {
     const float inv = 1.f / den;
     reinterpret_cast<float4*>(a.out + (int64_t)col * D)[tid] =
         make_float4(num.x * inv, num.y * inv, num.z * inv, num.w * inv);
+    if (a.ml_out && tid == 0) a.ml_out[col] = make_float2(mx, den);
   }
 }
 

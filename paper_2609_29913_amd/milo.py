@@ -29,12 +29,22 @@ MILO_P_INT8 = 1
 MILO_PATH_LATENT = 0
 MILO_PATH_RECONSTRUCT = 1
 MILO_PATH_AUTO = 2
+MILO_KV_INT8 = 0
+MILO_KV_E4M3 = 1
+MILO_OUT_F32 = 0
+MILO_OUT_BF16 = 1
 
 
 class milo_cache_desc(ctypes.Structure):
     _fields_ = [("n_blocks", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("block_tokens", _c_i32p),
                 ("rank_k", _c_i32p), ("rank_v", _c_i32p), ("p_format", ctypes.c_int32)]
+
+
+class milo_pages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32), ("k_codes", ctypes.c_void_p),
+                ("v_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
 class MiloError(RuntimeError):
@@ -111,6 +121,21 @@ def lib() -> ctypes.CDLL:
         L.milo_cache_recon_blocks.restype = ctypes.c_int
         L.milo_cache_set_rope.argtypes = [vp, ctypes.c_double, ctypes.POINTER(ctypes.c_int64)]
         L.milo_cache_set_rope.restype = ctypes.c_int
+        i32, i64 = ctypes.c_int32, ctypes.c_int64
+        pp = ctypes.POINTER(milo_pages)
+        L.milo_pages_plan_work.argtypes = [i32]
+        L.milo_pages_plan_work.restype = i64
+        L.milo_pages_plan.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+        L.milo_pages_plan.restype = ctypes.c_int
+        L.milo_pages_store.argtypes = [pp, vp, i64, vp, i64, vp, i32, vp]
+        L.milo_pages_store.restype = ctypes.c_int
+        L.milo_pages_load.argtypes = [pp, vp, i32, vp, i64, vp, i64, vp]
+        L.milo_pages_load.restype = ctypes.c_int
+        L.milo_attend_pages_work.argtypes = [i32, i32, i32, ctypes.c_int]
+        L.milo_attend_pages_work.restype = i64
+        L.milo_attend_pages.argtypes = [vp, _c_i32p, i32, pp, vp, i32, vp, vp, i32, vp, i64, i32, i32, i32,
+                                        ctypes.c_float, vp, i32, vp, vp]
+        L.milo_attend_pages.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -404,6 +429,213 @@ def milo_block_factors(blocks, vt, ranks, stream=None):
     _check(lib().milo_block_factors(ptrs, _i32(tokens), len(blocks), D, vt.data_ptr(), _i32(ranks), pp, rp,
                                     _stream(stream)))
     return ps, rs
+
+
+# ---- paged 8-bit cache ---------------------------------------------------------------------
+
+class MiloPages:
+    """A pool of 8-bit pages (milo_pages of include/milo.h): k_codes / v_codes
+    [n_pages][H_kv][page_tokens * d] (int8: MILO_KV_INT8, float8_e4m3fn: MILO_KV_E4M3) and
+    k_scale / v_scale float32 [n_pages][H_kv], contiguous tensors on one GPU, kept alive by
+    this object."""
+
+    def __init__(self, k_codes, v_codes, k_scale, v_scale, page_tokens: int):
+        import torch
+        fmt = {torch.int8: MILO_KV_INT8, torch.float8_e4m3fn: MILO_KV_E4M3}
+        for name, x in (("k_codes", k_codes), ("v_codes", v_codes)):
+            if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in fmt or x.dim() != 3 or \
+                    not x.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous int8 or float8_e4m3fn GPU tensor [n_pages][H_kv][page_tokens * d]")
+        if v_codes.shape != k_codes.shape or v_codes.dtype != k_codes.dtype or v_codes.device != k_codes.device:
+            raise ValueError("k_codes and v_codes differ in shape, dtype or device")
+        for name, x in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if not isinstance(x, torch.Tensor) or x.dtype != torch.float32 or not x.is_contiguous() or \
+                    x.device != k_codes.device or tuple(x.shape) != tuple(k_codes.shape[:2]):
+                raise ValueError(f"{name} must be a contiguous float32 tensor {tuple(k_codes.shape[:2])} on {k_codes.device}")
+        self.page_tokens = int(page_tokens)
+        self.n_pages, self.n_kv_heads = int(k_codes.shape[0]), int(k_codes.shape[1])
+        if self.page_tokens < 1 or k_codes.shape[2] % self.page_tokens:
+            raise ValueError(f"pages of {k_codes.shape[2]} codes per head do not hold {page_tokens} tokens")
+        self.head_dim = int(k_codes.shape[2]) // self.page_tokens
+        self.k_codes, self.v_codes, self.k_scale, self.v_scale = k_codes, v_codes, k_scale, v_scale
+        self.device = k_codes.device
+        self._c = milo_pages(self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, fmt[k_codes.dtype],
+                             k_codes.data_ptr(), v_codes.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self._as_parameter_ = ctypes.pointer(self._c)
+
+
+def milo_pages_create(n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, fmt: int = MILO_KV_INT8,
+                      device=None) -> MiloPages:
+    """A zeroed pool on the GPU (fmt: MILO_KV_INT8 or MILO_KV_E4M3)."""
+    import torch
+    if fmt not in (MILO_KV_INT8, MILO_KV_E4M3):
+        raise ValueError(f"fmt must be MILO_KV_INT8 or MILO_KV_E4M3, got {fmt}")
+    dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    shape = (int(n_pages), int(n_kv_heads), int(page_tokens) * int(head_dim))
+    dtype = torch.int8 if fmt == MILO_KV_INT8 else torch.float8_e4m3fn
+    codes = [torch.zeros(shape, dtype=torch.int8, device=dev).view(dtype) for _ in range(2)]
+    scales = [torch.zeros(shape[:2], dtype=torch.float32, device=dev) for _ in range(2)]
+    return MiloPages(*codes, *scales, page_tokens)
+
+
+def _pages_arg(pages) -> MiloPages:
+    import torch
+    if not isinstance(pages, MiloPages):
+        raise ValueError(f"pages must be a MiloPages, got {type(pages).__name__}")
+    if pages.device.index != torch.cuda.current_device():
+        raise ValueError(f"pages are on {pages.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return pages
+
+
+def _i32_dev(x, name: str, shape=None):
+    """A contiguous int32 tensor on the current GPU, of the given shape (-1: any)."""
+    _dev_tensor(x, name, ("torch.int32",), None if shape is None else len(shape))
+    if shape is not None and any(w >= 0 and w != n for w, n in zip(shape, x.shape)):
+        raise ValueError(f"{name} has shape {tuple(x.shape)}, expected {tuple(shape)}")
+    return x
+
+
+def _row_stride(x, name: str, heads: int, d: int) -> int:
+    """Row stride (elements) of bf16 rows [n][heads][d] whose rows may lie apart."""
+    import torch
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a tensor on the current GPU")
+    if str(x.dtype) not in _BF16_DTYPES:
+        raise ValueError(f"{name} must have dtype {' or '.join(_BF16_DTYPES)}, got {x.dtype}")
+    if x.dim() != 3 or tuple(x.shape[1:]) != (heads, d):
+        raise ValueError(f"{name} must be [n][{heads}][{d}], got {tuple(x.shape)}")
+    if x.shape[0] == 0:
+        return heads * d
+    if x.stride(2) != 1 or (heads > 1 and x.stride(1) != d):
+        raise ValueError(f"{name}'s rows of [{heads}][{d}] must be contiguous (strides {x.stride()})")
+    return int(x.stride(0)) if x.shape[0] > 1 else heads * d
+
+
+def _on_stream(stream):
+    """A context in which torch allocates on `stream` (None: as it is), so that memory made
+    for a call is neither still in use by, nor handed on to, another stream's work."""
+    import contextlib
+
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    if stream.device.index != torch.cuda.current_device():
+        raise ValueError(f"stream is on {stream.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return torch.cuda.stream(stream)
+
+
+def milo_pages_plan(lens, delta, page_tokens: int, table, ring, ring_state, n_slots: int | None = None, *,
+                    lens_out=None, ring_state_out=None, starts=None, slots=None, status=None, work=None, stream=None):
+    """Lengths, pages and slots of a step, on the GPU (milo_pages_plan of include/milo.h).
+    lens, delta int32 [n_req]; table [n_req][width] and ring [n_pages] are updated in place;
+    ring_state [2] (head, count).  Returns (lens_out, starts, slots, ring_state_out, status),
+    made here where not given; slots has n_slots entries.  work: int32 tensor of at least
+    milo_pages_plan_work(n_req) bytes, or None."""
+    import torch
+    n_req = int(lens.shape[0]) if isinstance(lens, torch.Tensor) and lens.dim() == 1 else -1
+    if n_req < 0:
+        raise ValueError("lens must be an int32 GPU tensor [n_req]")
+    _i32_dev(lens, "lens", (n_req,))
+    _i32_dev(delta, "delta", (n_req,))
+    _i32_dev(table, "table", (n_req, -1))
+    _i32_dev(ring, "ring", (-1,))
+    _i32_dev(ring_state, "ring_state", (2,))
+    if slots is None:
+        if n_slots is None:
+            raise ValueError("give slots, or n_slots for a new one")
+    elif n_slots is not None and n_slots != slots.shape[0]:
+        raise ValueError(f"slots has {slots.shape[0]} entries, n_slots is {n_slots}")
+    with _on_stream(stream):
+        def made(x, name, n):
+            return torch.empty(n, dtype=torch.int32, device=lens.device) if x is None else _i32_dev(x, name, (n,))
+        lens_out = made(lens_out, "lens_out", n_req)
+        ring_state_out = made(ring_state_out, "ring_state_out", 2)
+        starts = made(starts, "starts", n_req + 1)
+        slots = made(slots, "slots", int(n_slots) if slots is None else -1)
+        status = made(status, "status", 1)
+        need = lib().milo_pages_plan_work(n_req)
+        if work is None:
+            work = torch.empty(need // 4, dtype=torch.int32, device=lens.device)
+    if _i32_dev(work, "work").numel() * 4 < need:
+        raise ValueError(f"work holds {work.numel() * 4} bytes, {need} are needed")
+    _check(lib().milo_pages_plan(
+        lens.data_ptr(), delta.data_ptr(), n_req, int(page_tokens), table.data_ptr(), int(table.shape[1]), ring.data_ptr(),
+        int(ring.shape[0]), ring_state.data_ptr(), ring_state_out.data_ptr(), lens_out.data_ptr(), starts.data_ptr(),
+        slots.data_ptr(), int(slots.shape[0]), status.data_ptr(), work.data_ptr(), _stream(stream)))
+    return lens_out, starts, slots, ring_state_out, status
+
+
+def milo_pages_store(pages: MiloPages, k, v, slots, stream=None) -> None:
+    """Quantise rows k, v (bf16 [n][H_kv][d]; rows may lie apart) into their slots (int32 [n])."""
+    p = _pages_arg(pages)
+    ks, vs = _row_stride(k, "k", p.n_kv_heads, p.head_dim), _row_stride(v, "v", p.n_kv_heads, p.head_dim)
+    if v.shape[0] != k.shape[0]:
+        raise ValueError(f"k has {k.shape[0]} rows, v {v.shape[0]}")
+    _i32_dev(slots, "slots", (int(k.shape[0]),))
+    _check(lib().milo_pages_store(p._as_parameter_, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(), int(k.shape[0]),
+                                  _stream(stream)))
+
+
+def milo_pages_load(pages: MiloPages, slots, k_out=None, v_out=None, stream=None) -> None:
+    """Rows of `slots` (int32 [n]) back to bf16 into k_out and / or v_out [n][H_kv][d]."""
+    p = _pages_arg(pages)
+    _i32_dev(slots, "slots", (-1,))
+    if k_out is None and v_out is None:
+        raise ValueError("k_out and v_out are both None")
+    strides = [0, 0]
+    for i, (name, x) in enumerate((("k_out", k_out), ("v_out", v_out))):
+        if x is not None:
+            strides[i] = _row_stride(x, name, p.n_kv_heads, p.head_dim)
+            if x.shape[0] != slots.shape[0]:
+                raise ValueError(f"{name} has {x.shape[0]} rows, slots {slots.shape[0]}")
+            if x.shape[0] > 1 and strides[i] < p.n_kv_heads * p.head_dim:
+                raise ValueError(f"{name}'s rows overlap")
+    _check(lib().milo_pages_load(p._as_parameter_, slots.data_ptr(), int(slots.shape[0]), _addr(k_out), strides[0],
+                                 _addr(v_out), strides[1], _stream(stream)))
+
+
+def milo_attend_pages(pages: MiloPages, page_table, lens, q, scale: float, out, *, q_starts=None, causal: bool = True,
+                      cache: int | None = None, block_table=None, work=None, stream=None) -> None:
+    """Attention of q (bf16 [n_tok][H_q][d]; rows may lie apart) over each request's pages:
+    page_table int32 [n_req][width], lens int32 [n_req], q_starts int32 [n_req + 1] (None: one
+    query per request); out float32 or bfloat16 [n_tok][H_q][d].  causal: a request's queries
+    are its last rows; False: every query sees all of them.  cache and block_table add selected
+    blocks of a compressed context to every query's keys.  work: uint8 tensor of at least
+    milo_attend_pages_work(...) bytes, or None."""
+    import torch
+    p = _pages_arg(pages)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a bf16 GPU tensor [n_tok][H_q][d]")
+    n_tok, h_q = int(q.shape[0]), int(q.shape[1])
+    q_stride = _row_stride(q, "q", h_q, p.head_dim)
+    _dev_tensor(out, "out", ("torch.float32", "torch.bfloat16"), 3)
+    if out.shape != q.shape:
+        raise ValueError(f"out shape {tuple(out.shape)} differs from q shape {tuple(q.shape)}")
+    _i32_dev(lens, "lens", (-1,))
+    n_req = int(lens.shape[0])
+    _i32_dev(page_table, "page_table", (n_req, -1))
+    if q_starts is not None:
+        _i32_dev(q_starts, "q_starts", (n_req + 1,))
+    table = None if block_table is None else np.asarray(block_table, dtype=np.int32).reshape(-1)
+    n_sel = 0 if table is None else int(table.size)
+    if cache is None:
+        if n_sel:
+            raise ValueError("block_table without a cache")
+    elif cache not in _CACHES:
+        raise ValueError("unknown cache handle (not created by milo_cache_create, or already freed)")
+    need = lib().milo_attend_pages_work(n_tok, h_q, p.head_dim, 1 if n_sel else 0)
+    if work is None:
+        with _on_stream(stream):
+            work = torch.empty(need, dtype=torch.uint8, device=q.device)
+    elif _dev_tensor(work, "work", ("torch.uint8",)).numel() < need:
+        raise ValueError(f"work holds {work.numel()} bytes, {need} are needed")
+    _check(lib().milo_attend_pages(
+        ctypes.c_void_p(cache), _i32(table) if n_sel else None, n_sel, p._as_parameter_, page_table.data_ptr(),
+        int(page_table.shape[1]), lens.data_ptr(), _addr(q_starts), n_req, q.data_ptr(), q_stride, n_tok, h_q,
+        1 if causal else 0, float(scale), out.data_ptr(), MILO_OUT_F32 if out.dtype == torch.float32 else MILO_OUT_BF16,
+        work.data_ptr(), _stream(stream)))
 
 
 def milo_cache_free(cache: int | None) -> None:
