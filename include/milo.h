@@ -463,11 +463,13 @@ int milo_pages_load(const milo_pages* pages, const int32_t* slots, int32_t n_tok
  *   work         milo_attend_pages_work bytes, 256-byte aligned: this call's alone until
  *                its work has run.
  * Scores, softmax sums and outputs are accumulated in fp32 from the exact codes; the
- * weights enter the value product in bf16 (2^-9), in two parts (2^-17) for fp32 output.
+ * weights enter the value product in bf16 for bf16 output, in three bf16 parts (all of
+ * their 24 bits) for fp32 output.
  * Errors: INVALID_ARG, UNSUPPORTED, and with a cache those of milo_attend_decode. */
 #define MILO_OUT_F32 0
 #define MILO_OUT_BF16 1
-int64_t milo_attend_pages_work(int32_t n_tok, int32_t n_q_heads, int32_t head_dim, int with_cache);
+int64_t milo_attend_pages_work(int32_t n_req, int32_t n_tok, int32_t n_q_heads, int32_t n_kv_heads,
+                               int32_t head_dim, int with_cache);
 int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_sel,
                       const milo_pages* pages, const int32_t* page_table, int32_t table_width,
                       const int32_t* lens, const int32_t* q_starts, int32_t n_req, const uint16_t* q,

@@ -74,6 +74,97 @@ inline int check_rows(const char* name, const void* p, int64_t stride, int64_t w
   return MILO_OK;
 }
 
+// ---- the work of an attention call, in rows ---------------------------------------
+// Request r's m queries are cut into column tiles of tt tokens; tile k sees vis(k) of
+// its n rows.  Positions number the work: request by request, KV head by KV head, tile
+// by tile, each tile kTileCost + vis(k) long (requests without queries take none).
+// Share w of W has the positions [w X / W, (w + 1) X / W) of X, in whatever tiles they
+// fall, so lengths may differ as they like; a tile's rows are cut at multiples of
+// kRowAlign.  All of it follows from the lengths, on the device.
+constexpr int kRowAlign = 64;
+constexpr int kTileCost = 128;  // what a tile costs besides its rows
+
+struct Request {
+  int start, m, n;  // first query, queries, rows held
+};
+
+// rows that query number j - 1 of the request sees (at most its last one's)
+__host__ __device__ inline int seen_upto(const Request& q, int j, int causal) {
+  if (!causal) return q.n;
+  const int v = q.n - q.m + (j < q.m ? j : q.m);
+  return v > 0 ? v : 0;
+}
+
+// positions of the first k of a request's tiles
+__host__ __device__ inline int64_t tiles_cost(const Request& q, int k, int tt, int causal) {
+  if (k <= 0) return 0;
+  if (!causal) return (int64_t)k * (kTileCost + q.n);
+  // tile i sees max(0, base + (i + 1) tt) rows, the request's last tile n
+  const int all = (q.m + tt - 1) / tt, whole = k < all ? k : all - 1;
+  const int64_t base = (int64_t)q.n - q.m;
+  int64_t skip = base < 0 ? -base / tt : 0;  // tiles that see nothing
+  if (skip > whole) skip = whole;
+  int64_t sum = (whole - skip) * base + (int64_t)tt * (whole * ((int64_t)whole + 1) / 2 - skip * (skip + 1) / 2);
+  if (k >= all) sum += q.n;
+  return sum + (int64_t)k * kTileCost;
+}
+__host__ __device__ inline int64_t request_cost(const Request& q, int tt, int causal) {
+  return tiles_cost(q, (q.m + tt - 1) / tt, tt, causal);
+}
+
+__host__ __device__ inline int64_t share_begin(int w, int64_t X, int W) { return w * X / W; }
+// the share that holds position p: the largest w with floor(w X / W) <= p
+__host__ __device__ inline int share_holding(int64_t p, int64_t X, int W) { return (int)(((p + 1) * W + X - 1) / X) - 1; }
+
+// the row at which boundary b cuts the tile at positions [p0, p1) that sees vis rows
+__host__ __device__ inline int row_at(int64_t b, int64_t p0, int64_t p1, int vis) {
+  if (b <= p0 + kTileCost) return 0;
+  if (b >= p1) return vis;
+  return (int)(b - p0 - kTileCost) & ~(kRowAlign - 1);
+}
+
+struct Place {
+  int r, head, tile;
+  int64_t p;   // first position of the tile
+  Request rq;
+};
+
+// the tile that holds position b, where request r0's work begins at p <= b
+template <typename Get>
+__host__ __device__ inline Place place_of(const Get& get, int r0, int64_t p, int64_t b, int H, int tt, int causal) {
+  Place at;
+  int64_t cost;
+  for (at.r = r0;; ++at.r) {
+    at.rq = get(at.r);
+    cost = request_cost(at.rq, tt, causal);
+    if (b < p + H * cost) break;
+    p += H * cost;
+  }
+  at.head = (int)((b - p) / cost);
+  p += at.head * cost;
+  int t0 = 0, t1 = (at.rq.m + tt - 1) / tt;
+  while (t1 - t0 > 1) {
+    const int mid = (t0 + t1) >> 1;
+    if (p + tiles_cost(at.rq, mid, tt, causal) <= b) t0 = mid;
+    else t1 = mid;
+  }
+  at.tile = t0;
+  at.p = p + tiles_cost(at.rq, t0, tt, causal);
+  return at;
+}
+
+// the tile after, which begins at p (there is one)
+template <typename Get>
+__host__ __device__ inline void next_tile(const Get& get, Place& at, int64_t p, int H, int tt) {
+  at.p = p;
+  if (++at.tile < (at.rq.m + tt - 1) / tt) return;
+  at.tile = 0;
+  if (++at.head < H) return;
+  at.head = 0;
+  do at.rq = get(++at.r);
+  while (at.rq.m == 0);
+}
+
 #ifdef __HIPCC__
 
 __device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }

@@ -1,6 +1,7 @@
 // Attention over the paged 8-bit cache (include/milo.h: milo_attend_pages).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "milo_attend.h"
@@ -19,7 +20,12 @@ struct PagesArgs {
   const float* ctx_o;      // [n_tok * H_q][d] attention over the compressed context (NULL: none)
   const float2* ctx_ml;    // its maximum in log2 units and its sum
   int64_t q_stride;
+  float* part_o;           // [2 grid][columns of a tile][d] parts of tiles that workgroups share
+  float2* part_ml;         // their maxima (log2 units) and sums
+  int4* meta;              // [grid] the tile that begins in a workgroup and ends in a later one
   float qscale;            // scale * log2(e)
+  int32_t min_rows;        // positions a workgroup gets at least,
+  int32_t min_wgs;         // unless fewer workgroups than this would work
   int32_t n_req, n_tok, H_q, G, width, lg_page, causal, out_bf16;
 };
 
@@ -27,84 +33,516 @@ __device__ inline int start_of(const PagesArgs& a, int i) {
   return a.starts ? min(max(a.starts[i], 0), a.n_tok) : i;
 }
 
-// Rows a query sees: all n of its request, or, as query j of m, its own and those before.
-__device__ inline int seen_by(const PagesArgs& a, int n, int j, int m) { return a.causal ? max(0, n - m + j + 1) : n; }
 
-template <int D, int FMT>
-__global__ __launch_bounds__(64) void pages_simple_kernel(PagesArgs a) {
-  __shared__ float qs[D], ps[64];
-  const int lane = threadIdx.x, h = blockIdx.y, g = h / a.G, P = 1 << a.lg_page;
-  const int t = blockIdx.x;
-  // the request: the last with start <= t
-  int lo = 0, hi = a.n_req;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (start_of(a, mid) <= t) lo = mid;
-    else hi = mid;
-  }
-  const int s0 = start_of(a, lo), s1 = a.starts ? start_of(a, lo + 1) : lo + 1;
-  if (t < s0 || t >= s1) return;
-  const int64_t cap = (int64_t)a.width << a.lg_page;
-  const int n = (int)min((int64_t)max(a.lens[lo], 0), cap);
-  const int seen = seen_by(a, n, t - s0, s1 - s0);
-  for (int c = lane; c < D; c += 64) qs[c] = bf16_value(a.q[(int64_t)t * a.q_stride + (int64_t)h * D + c]);
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, o[D / 64] = {};
-  for (int r0 = 0; r0 < seen; r0 += 64) {
-    const int r = r0 + lane;
-    float s = -INFINITY;
-    if (r < seen) {
-      const int id = a.table[(int64_t)lo * a.width + (r >> a.lg_page)];
-      if ((uint32_t)id < (uint32_t)a.p.n_pages) {
-        const int64_t ph = (int64_t)id * a.p.n_kv_heads + g;
-        const uint8_t* kc = (const uint8_t*)a.p.k_codes + ph * P * D;
-        float dot = 0.f;
-        for (int c = 0; c < D; c += 4) {
-          const float4 x = code_values<FMT>(*(const uint32_t*)(kc + key_byte(r & (P - 1), c, D)));
-          dot += x.x * qs[c] + x.y * qs[c + 1] + x.z * qs[c + 2] + x.w * qs[c + 3];
-        }
-        s = dot * (a.p.k_scale[ph] * a.qscale);
-      } else {
-        s = __uint_as_float(0x7FC00000u);
-      }
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kPagesThreads = 256;   // four waves
+constexpr int kPagesWaves = kPagesThreads / 64;
+
+// eight codes as bf16, exactly
+template <int FMT>
+__device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi) {
+  bf16x8 v;
+  if constexpr (FMT == MILO_KV_INT8) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = (__bf16)(float)(int8_t)(lo >> (8 * e));
+      v[4 + e] = (__bf16)(float)(int8_t)(hi >> (8 * e));
     }
-    float mx = s;
-    for (int k = 32; k > 0; k >>= 1) mx = fmaxf(mx, __shfl_xor(mx, k));
-    mx = fmaxf(mx, m);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    const float p = exp2f(s - ref), f = exp2f(m - ref);
-    float sum = p;
-    for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
-    l = l * f + sum;
-    m = mx;
-    __syncthreads();
-    ps[lane] = p;
-    __syncthreads();
-    for (int k = 0; k < D / 64; ++k) o[k] *= f;
-    for (int u = 0; u < 64 && r0 + u < seen; ++u) {
-      const int rr = r0 + u, id = a.table[(int64_t)lo * a.width + (rr >> a.lg_page)];
-      if ((uint32_t)id >= (uint32_t)a.p.n_pages) continue;
-      const int64_t ph = (int64_t)id * a.p.n_kv_heads + g;
-      const uint8_t* vc = (const uint8_t*)a.p.v_codes + ph * P * D;
-      const float w = ps[u] * a.p.v_scale[ph];
-      for (int k = 0; k < D / 64; ++k) o[k] += w * code_values<FMT>(vc[value_byte(rr & (P - 1), lane + 64 * k, D)]).x;
-    }
+  } else {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
+    const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+    v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1];
+    v[4] = c[0]; v[5] = c[1]; v[6] = d[0]; v[7] = d[1];
   }
-  const int64_t col = (int64_t)t * a.H_q + h;
+  return v;
+}
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int lane_of(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
+__device__ __forceinline__ float lane_of(float v, int l) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l));
+}
+
+__device__ inline Request request_of(const PagesArgs& a, int r) {
+  Request q;
+  q.start = start_of(a, r);
+  q.m = a.starts ? max(0, start_of(a, r + 1) - q.start) : 1;
+  q.n = (int)min((int64_t)max(a.lens[r], 0), (int64_t)a.width << a.lg_page);
+  return q;
+}
+
+// merges a column's result with the compressed context's and stores 4 dims of it
+__device__ inline void finish(const PagesArgs& a, int64_t col, int d, int D, float m, float l, float4 o) {
   if (a.ctx_ml) {
     const float2 cm = a.ctx_ml[col];
-    const float mx = fmaxf(m, cm.x), fp = m == -INFINITY && l == 0.f ? 0.f : exp2f(m - mx), fc = exp2f(cm.x - mx) * cm.y;
+    const float4 co = *reinterpret_cast<const float4*>(a.ctx_o + col * D + d);
+    const float mx = fmaxf(m, cm.x);
+    const float fp = m == -INFINITY ? (l == 0.f ? 0.f : l) : exp2_hw(m - mx), fc = exp2_hw(cm.x - mx) * cm.y;
     l = l * fp + fc;
-    for (int k = 0; k < D / 64; ++k) o[k] = o[k] * fp + fc * a.ctx_o[col * D + lane + 64 * k];
+    o.x = o.x * fp + co.x * fc;
+    o.y = o.y * fp + co.y * fc;
+    o.z = o.z * fp + co.z * fc;
+    o.w = o.w * fp + co.w * fc;
   }
-  for (int k = 0; k < D / 64; ++k) {
-    const float x = l == 0.f ? 0.f : o[k] / l;
-    if (a.out_bf16) ((uint16_t*)a.out)[col * D + lane + 64 * k] = (uint16_t)bf16_bits(x);
-    else ((float*)a.out)[col * D + lane + 64 * k] = x;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  o.x *= inv;
+  o.y *= inv;
+  o.z *= inv;
+  o.w *= inv;
+  if (a.out_bf16) {
+    uint2 w;
+    w.x = bf16_bits(o.x) | bf16_bits(o.y) << 16;
+    w.y = bf16_bits(o.z) | bf16_bits(o.w) << 16;
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + col * D + d) = w;
+  } else {
+    *reinterpret_cast<float4*>(static_cast<float*>(a.out) + col * D + d) = o;
+  }
+}
+
+// Pages of one request as a wave reads them: lane i holds the id and scales of page
+// base + i, so a step takes them without waiting for memory.
+struct Window {
+  int base, id;
+  float ks, vs;
+};
+
+__device__ inline Window window_at(const PagesArgs& a, int req, int head, int base, int last_page) {
+  Window w;
+  w.base = base;
+  const int pg = min(base + (int)(threadIdx.x & 63), last_page);
+  const int id = a.table[(int64_t)req * a.width + pg];
+  const bool in = (uint32_t)id < (uint32_t)a.p.n_pages;
+  w.id = in ? id : 0;
+  const int64_t at = (int64_t)w.id * a.p.n_kv_heads + head;
+  const float nan = __uint_as_float(0x7FC00000u);
+  w.ks = in ? a.p.k_scale[at] : nan;
+  w.vs = in ? a.p.v_scale[at] : nan;
+  return w;
+}
+
+// One step's codes (GS groups of 16 rows) and scales.
+template <int D, int GS>
+struct Step {
+  uint4 k[GS][D / 64], v[GS][D / 64];
+  float ks[GS], vs[GS];
+};
+
+template <int D, int GS>
+__device__ __forceinline__ void load_step(const PagesArgs& a, int req, int head, Window& w, int row, int last_page,
+                                          Step<D, GS>& st) {
+  const int P = 1 << a.lg_page, lane = threadIdx.x & 63;
+  if ((row >> a.lg_page) - w.base >= 64) w = window_at(a, req, head, row >> a.lg_page, last_page);
+  const int64_t head_bytes = (int64_t)P * D, page_bytes = head_bytes * a.p.n_kv_heads;
+#pragma unroll
+  for (int g = 0; g < GS; ++g) {
+    const int r = row + 16 * g, pg = min(r >> a.lg_page, last_page), li = min(pg - w.base, 63);
+    const int id = lane_of(w.id, li);
+    st.ks[g] = lane_of(w.ks, li);
+    st.vs[g] = lane_of(w.vs, li);
+    const int64_t at = id * page_bytes + head * head_bytes + (r & (P - 1)) * D;
+    const uint8_t* kp = static_cast<const uint8_t*>(a.p.k_codes) + at;
+    const uint8_t* vp = static_cast<const uint8_t*>(a.p.v_codes) + at;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      st.k[g][j] = *reinterpret_cast<const uint4*>(kp + 1024 * j + 16 * lane);
+      st.v[g][j] = *reinterpret_cast<const uint4*>(vp + 1024 * j + 16 * lane);
+    }
+  }
+}
+
+// A wave's running softmax over NT tiles of 16 columns: lane (n = l % 16, q = l / 16)
+// holds of column n the maximum (all four q alike), its own part of the sum, and dims
+// 16 t + 4 q .. + 3 of the outputs.
+template <int D, int NT>
+struct Running {
+  f32x4 o[NT][D / 16];
+  float m[NT], l[NT];
+};
+
+// Adds a step's rows.  Scores: 16x16x32 products keys x queries, so lane (n, q) holds
+// rows 4 q .. 4 q + 3 of each group for column n; two groups' weights are, as they
+// stand, the right operand of the product with the values' 32 rows in the order the
+// codes are stored in.  The reference that weights are taken relative to moves only
+// when a score passes it by 2^8, which fp32 sums bear.
+template <int D, int FMT, int PARTS, int NT, int GS>
+__device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&qf)[NT][D / 32], float qscale, int row,
+                                         int n, const int (&vis)[NT], bool masked, Running<D, NT>& run) {
+  const int lane = threadIdx.x & 63, q4 = (lane >> 4) * 4;
+  f32x4 s[GS][NT];
+#pragma unroll
+  for (int g = 0; g < GS; ++g) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) s[g][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      const bf16x8 a0 = codes_bf16<FMT>(st.k[g][j].x, st.k[g][j].y), a1 = codes_bf16<FMT>(st.k[g][j].z, st.k[g][j].w);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[g][t] = mfma16(a0, qf[t][2 * j], s[g][t]);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[g][t] = mfma16(a1, qf[t][2 * j + 1], s[g][t]);
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < GS; ++g)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[g][t][i] *= st.ks[g] * qscale;
+  if (masked) {
+#pragma unroll
+    for (int g = 0; g < GS; ++g)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (row + 16 * g + q4 + i >= vis[t]) s[g][t][i] = -INFINITY;
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    float mx = s[0][t][0];
+#pragma unroll
+    for (int g = 0; g < GS; ++g)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[g][t][i]);
+    if (__any(mx > run.m[t] + 8.f)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      mx = fmaxf(mx, run.m[t]);
+      const float f = mx == -INFINITY ? 1.f : exp2_hw(run.m[t] - mx);
+      run.m[t] = mx;
+      run.l[t] *= f;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) run.o[t][c] *= f;
+    }
+  }
+  bf16x8 w[GS / 2][NT][PARTS];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const float ref = run.m[t] == -INFINITY ? 0.f : run.m[t];
+    float sum = 0.f;
+#pragma unroll
+    for (int g = 0; g < GS; ++g)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x = exp2_hw(s[g][t][i] - ref);
+        sum += x;
+        x *= st.vs[g];
+        // a page of NaN that a column does not see must not reach it
+        if (masked && row + 16 * g + q4 + i >= vis[t]) x = 0.f;
+        const int e = (g & 1) * 4 + i;
+        if constexpr (PARTS == 1) {
+          w[g / 2][t][0][e] = (__bf16)x;  // 2^-9
+        } else {  // three bf16 hold all 24 bits
+          const float h = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u), r = x - h;
+          const float h2 = __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
+          w[g / 2][t][0][e] = (__bf16)h;
+          w[g / 2][t][1][e] = (__bf16)h2;
+          w[g / 2][t][2][e] = (__bf16)(r - h2);
+        }
+      }
+    run.l[t] += sum;
+  }
+#pragma unroll
+  for (int g = 0; g < GS; g += 2) {
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      uint32_t va[4] = {st.v[g][j].x, st.v[g][j].y, st.v[g][j].z, st.v[g][j].w};
+      uint32_t vb[4] = {st.v[g + 1][j].x, st.v[g + 1][j].y, st.v[g + 1][j].z, st.v[g + 1][j].w};
+      if (FMT == MILO_KV_E4M3 && masked) {  // rows behind the request's last hold anything, NaN among it
+        const int na = min(max(n - row - 16 * g - q4, 0), 4), nb = min(max(n - row - 16 * g - 16 - q4, 0), 4);
+        const uint32_t ka = na == 4 ? ~0u : (1u << 8 * na) - 1u, kb = nb == 4 ? ~0u : (1u << 8 * nb) - 1u;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          va[c] &= ka;
+          vb[c] &= kb;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const bf16x8 vf = codes_bf16<FMT>(va[c], vb[c]);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) run.o[t][4 * j + c] = mfma16(vf, w[g / 2][t][p], run.o[t][4 * j + c]);
+      }
+    }
+  }
+}
+
+// SHARE: the workgroup's waves split a tile's rows (16 NT columns), else its columns
+// (64 NT columns, every wave reads all rows).
+template <int D, int FMT, int PARTS, int NT, bool SHARE>
+__global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(PagesArgs a) {
+  constexpr int GS = NT == 1 ? 4 : 2, ROWS = 16 * GS;
+  constexpr int COLS = SHARE ? 16 * NT : 16 * NT * kPagesWaves;
+  constexpr int OS = D + 4;  // row stride of a column's partial in LDS
+  __shared__ int64_t pre[kPagesThreads + 1];
+  // two sets in turn: a wave writes a tile's while others still read the last one's
+  __shared__ float joined[2][2][kPagesWaves][16 * NT];
+  __shared__ __align__(16) float part[SHARE ? kPagesWaves * 16 * NT * OS : 4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int tt = COLS / a.G, H = a.p.n_kv_heads;
+
+  // the call's work and this workgroup's share of it
+  const int chunk = (a.n_req + kPagesThreads - 1) / kPagesThreads;
+  {
+    int64_t own = 0;
+    for (int r = tid * chunk; r < min((tid + 1) * chunk, a.n_req); ++r) {
+      own += request_cost(request_of(a, r), tt, a.causal);
+    }
+    int64_t inc = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t up = __shfl_up(inc, o);
+      if (lane >= o) inc += up;
+    }
+    if (lane == 63) pre[1 + tid] = inc;
+    __syncthreads();
+    int64_t before = 0;
+    for (int w = 0; w < wave; ++w) before += pre[64 * (w + 1)];
+    __syncthreads();
+    if (tid == 0) pre[0] = 0;
+    pre[1 + tid] = before + inc;
+    __syncthreads();
+  }
+  const int64_t X = H * pre[kPagesThreads];
+  // (a share is at least kTileCost long, so none is empty)
+  int W = (int)min(min((int64_t)gridDim.x, X / kTileCost), max(X / a.min_rows, (int64_t)a.min_wgs));
+  if (W >= kXcds) W -= W % kXcds;
+  int4* meta = a.meta + blockIdx.x;
+  if (tid == 0) *meta = make_int4(-1, 0, 0, 0);
+  if ((int)blockIdx.x >= W || X == 0) return;
+  // consecutive shares on one XCD, whose L2 then holds the rows that tiles share
+  const int w = W >= kXcds ? (int)(blockIdx.x % kXcds) * (W / kXcds) + blockIdx.x / kXcds : blockIdx.x;
+  const int64_t b0 = share_begin(w, X, W), b1 = share_begin(w + 1, X, W);
+
+  // the tile that b0 falls in
+  Place at;
+  const auto get = [&](int r) { return request_of(a, r); };
+  {
+    int lo = 0, hi = kPagesThreads;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (H * pre[mid] <= b0) lo = mid;
+      else hi = mid;
+    }
+    at = place_of(get, lo * chunk, H * pre[lo], b0, H, tt, a.causal);
+  }
+  bool first = true;
+  int parity = 0;
+  for (int64_t pos = b0; pos < b1;) {
+    const int j0 = uniform(at.tile * tt), ntok = uniform(min(tt, at.rq.m - at.tile * tt)), n = uniform(at.rq.n);
+    const int req = uniform(at.r), g = uniform(at.head), start = uniform(at.rq.start), m = uniform(at.rq.m);
+    const int vis_hi = uniform(seen_upto(at.rq, j0 + ntok, a.causal));
+    const int64_t p0 = at.p, p1 = p0 + kTileCost + vis_hi;
+    const int ra = uniform(row_at(b0, p0, p1, vis_hi)), rb = uniform(row_at(b1, p0, p1, vis_hi));
+    const bool whole = b0 <= p0 && b1 >= p1;
+    const int slot = 2 * w + (first ? 0 : 1);
+
+    // this wave's rows and columns
+    const int col0 = SHARE ? 0 : wave * 16 * NT, ncol = ntok * a.G;
+    const int64_t q0 = (int64_t)(start + j0) * a.H_q + g * a.G;  // the tile's first column in out
+    int wa = ra, wb = rb;
+    if (SHARE) {
+      const int steps = (rb - ra + ROWS - 1) / ROWS;
+      wa = ra + steps * wave / kPagesWaves * ROWS;
+      wb = min(rb, ra + steps * (wave + 1) / kPagesWaves * ROWS);
+    }
+    Running<D, NT> run;
+    int vis[NT], vis_lo = n;
+    bf16x8 qf[NT][D / 32];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int c = col0 + 16 * t + (lane & 15), tok = c / a.G;
+      vis[t] = 0;
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) qf[t][k] = bf16x8{};
+      if (c < ncol) {
+        const Request me{start, m, n};
+        vis[t] = seen_upto(me, j0 + tok + 1, a.causal);
+        const uint16_t* src = a.q + (int64_t)(start + j0 + tok) * a.q_stride + (int64_t)(g * a.G + c % a.G) * D;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k)
+          qf[t][k] = *reinterpret_cast<const bf16x8*>(src + 64 * (k / 2) + 16 * (lane >> 4) + 8 * (k % 2));
+      }
+      run.m[t] = -INFINITY;
+      run.l[t] = 0.f;
+#pragma unroll
+      for (int c2 = 0; c2 < D / 16; ++c2) run.o[t][c2] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // steps below vis_lo need no mask: the fewest rows a column of this wave sees
+    if (col0 < ncol) {
+      const Request me{start, m, n};
+      vis_lo = seen_upto(me, j0 + col0 / a.G + 1, a.causal);
+    }
+    vis_lo = uniform(vis_lo);
+    wa = uniform(wa);
+    wb = uniform(wb);
+    if (wa < wb && col0 < ncol) {
+      const int last_page = (n - 1) >> a.lg_page;
+      Window win = window_at(a, req, g, wa >> a.lg_page, last_page);
+      Step<D, GS> s0, s1;
+      load_step(a, req, g, win, wa, last_page, s0);
+      for (int row = wa;;) {
+        if (row + ROWS < wb) load_step(a, req, g, win, row + ROWS, last_page, s1);
+        add_step<D, FMT, PARTS, NT, GS>(s0, qf, a.qscale, row, n, vis, row + ROWS > vis_lo, run);
+        if ((row += ROWS) >= wb) break;
+        if (row + ROWS < wb) load_step(a, req, g, win, row + ROWS, last_page, s0);
+        add_step<D, FMT, PARTS, NT, GS>(s1, qf, a.qscale, row, n, vis, row + ROWS > vis_lo, run);
+        if ((row += ROWS) >= wb) break;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      run.l[t] += __shfl_xor(run.l[t], 16);
+      run.l[t] += __shfl_xor(run.l[t], 32);
+    }
+    if (SHARE) {
+      auto& wave_m = joined[parity][0];
+      auto& wave_l = joined[parity][1];
+      parity ^= 1;
+      // join the waves: factors relative to the largest maximum, sums in wave order
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if (lane < 16) {
+          wave_m[wave][16 * t + lane] = run.m[t];
+          wave_l[wave][16 * t + lane] = run.l[t];
+        }
+      __syncthreads();
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int c = 16 * t + (lane & 15);
+        float mx = wave_m[0][c];
+#pragma unroll
+        for (int k = 1; k < kPagesWaves; ++k) mx = fmaxf(mx, wave_m[k][c]);
+        const float f = run.m[t] == -INFINITY ? 1.f : exp2_hw(run.m[t] - mx);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const f32x4 o = run.o[t][k] * f;
+          *reinterpret_cast<f32x4*>(&part[(wave * 16 * NT + c) * OS + 16 * k + 4 * (lane >> 4)]) = o;
+        }
+      }
+      __syncthreads();
+      for (int x = tid; x < ncol * (D / 4); x += kPagesThreads) {
+        const int c = x / (D / 4), d = x % (D / 4) * 4;
+        float mx = wave_m[0][c], l = 0.f;
+#pragma unroll
+        for (int k = 1; k < kPagesWaves; ++k) mx = fmaxf(mx, wave_m[k][c]);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kPagesWaves; ++k) {
+          const float wm = wave_m[k][c];
+          l += wave_l[k][c] * (wm == -INFINITY ? 1.f : exp2_hw(wm - mx));
+          const float4 y = *reinterpret_cast<const float4*>(&part[(k * 16 * NT + c) * OS + d]);
+          o.x += y.x;
+          o.y += y.y;
+          o.z += y.z;
+          o.w += y.w;
+        }
+        if (whole) {
+          finish(a, q0 + (int64_t)(c / a.G) * a.H_q + c % a.G, d, D, mx, l, o);
+        } else {
+          *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * COLS + c) * D + d) = o;
+          if (d == 0) a.part_ml[(int64_t)slot * COLS + c] = make_float2(mx, l);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int c = col0 + 16 * t + (lane & 15);
+        if (c < ncol) {
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const int d = 16 * k + 4 * (lane >> 4);
+            const float4 o = make_float4(run.o[t][k][0], run.o[t][k][1], run.o[t][k][2], run.o[t][k][3]);
+            if (whole) finish(a, q0 + (int64_t)(c / a.G) * a.H_q + c % a.G, d, D, run.m[t], run.l[t], o);
+            else *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * COLS + c) * D + d) = o;
+          }
+          if (!whole && lane < 16) a.part_ml[(int64_t)slot * COLS + c] = make_float2(run.m[t], run.l[t]);
+        }
+      }
+    }
+    // a tile that begins here and goes on in the next workgroups: joined afterwards
+    if (tid == 0 && b0 <= p0 && b1 < p1) {
+      const int we = share_holding(p1 - 1, X, W);
+      *meta = make_int4((int)q0, ncol, slot, we);
+    }
+    first = false;
+    pos = p1;
+    if (pos < b1) next_tile(get, at, p1, H, tt);
+  }
+}
+
+// Joins the parts of the tile that begins in share w and ends in share we: its own
+// slot and the first slot of the shares after it, in this order.
+template <int D, int COLS>
+__global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) {
+  constexpr int TPC = D / 4;  // threads of a column
+  const int4 mt = a.meta[blockIdx.x];
+  if (mt.x < 0) return;
+  const int s0 = mt.z, we = mt.w, w = s0 >> 1;
+  for (int x = blockIdx.y * kPagesThreads + threadIdx.x; x < mt.y * TPC; x += gridDim.y * kPagesThreads) {
+    const int c = x / TPC, d = x % TPC * 4;
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = w; k <= we; ++k) {
+      const int64_t at = (int64_t)(k == w ? s0 : 2 * k) * COLS + c;
+      const float2 ml = a.part_ml[at];
+      const float4 y = *reinterpret_cast<const float4*>(a.part_o + at * D + d);
+      if (ml.x == -INFINITY && ml.y == 0.f) continue;
+      const float mx = fmaxf(m, ml.x);
+      const float f = m == -INFINITY ? 1.f : exp2_hw(m - mx), fy = ml.x == -INFINITY ? 1.f : exp2_hw(ml.x - mx);
+      l = l * f + ml.y * fy;
+      o.x = o.x * f + y.x * fy;
+      o.y = o.y * f + y.y * fy;
+      o.z = o.z * f + y.z * fy;
+      o.w = o.w * f + y.w * fy;
+      m = mx;
+    }
+    finish(a, mt.x + (int64_t)(c / a.G) * a.H_q + c % a.G, d, D, m, l, o);
   }
 }
 
 int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
+
+constexpr int kGrid = 512;  // workgroups at most: two on every CU
+
+// Columns of a workgroup's tile: 16 where requests bring few queries each (the waves
+// split the rows), else 256 (the waves split the columns).
+bool few_columns(int32_t n_req, int32_t n_tok, int G) { return (int64_t)n_tok * G <= 32 * (int64_t)n_req; }
+int tile_columns(int32_t n_req, int32_t n_tok, int G) { return few_columns(n_req, n_tok, G) ? 16 : 64 * kPagesWaves; }
+
+template <int D, int FMT, int PARTS>
+void launch_pages(const PagesArgs& a, bool few, hipStream_t s) {
+  if (few) {
+    hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 1, true>), dim3(kGrid), dim3(kPagesThreads), 0, s, a);
+    hipLaunchKernelGGL((pages_join_kernel<D, 16>), dim3(kGrid, 2), dim3(kPagesThreads), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 4, false>), dim3(kGrid), dim3(kPagesThreads), 0, s, a);
+    hipLaunchKernelGGL((pages_join_kernel<D, 256>), dim3(kGrid, 16), dim3(kPagesThreads), 0, s, a);
+  }
+}
+
+template <int D>
+void launch_pages(const PagesArgs& a, bool few, hipStream_t s) {
+  const bool e4m3 = a.p.format == MILO_KV_E4M3;
+  if (a.out_bf16) {
+    if (e4m3) launch_pages<D, MILO_KV_E4M3, 1>(a, few, s);
+    else launch_pages<D, MILO_KV_INT8, 1>(a, few, s);
+  } else {
+    if (e4m3) launch_pages<D, MILO_KV_E4M3, 3>(a, few, s);
+    else launch_pages<D, MILO_KV_INT8, 3>(a, few, s);
+  }
+}
 
 }  // namespace
 }  // namespace milo
@@ -113,10 +551,13 @@ using namespace milo;
 
 extern "C" {
 
-int64_t milo_attend_pages_work(int32_t n_tok, int32_t n_q_heads, int32_t head_dim, int with_cache) {
-  if (n_tok < 0 || n_q_heads < 1 || head_dim < 1) return 0;
-  const int64_t cols = (int64_t)n_tok * n_q_heads;
-  return with_cache ? round256(cols * 8) + round256(cols * head_dim * 4) + 256 : 256;
+int64_t milo_attend_pages_work(int32_t n_req, int32_t n_tok, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                               int with_cache) {
+  if (n_req < 0 || n_tok < 0 || n_kv_heads < 1 || n_q_heads < n_kv_heads || head_dim < 1) return 0;
+  const int64_t cols = (int64_t)n_tok * n_q_heads, slot_cols = 2 * kGrid * tile_columns(n_req, n_tok, n_q_heads / n_kv_heads);
+  int64_t bytes = round256(kGrid * (int64_t)sizeof(int4)) + round256(slot_cols * 8) + round256(slot_cols * head_dim * 4);
+  if (with_cache) bytes += round256(cols * 8) + round256(cols * head_dim * 4);
+  return bytes;
 }
 
 int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_sel, const milo_pages* pages,
@@ -156,13 +597,22 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   if (!work || !aligned_to(work, 256)) return pages_fail(MILO_ERR_INVALID_ARG, "work must be non-NULL and 256-byte aligned");
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   PagesArgs a{};
+  const bool few = few_columns(n_req, n_tok, G);
+  const int64_t slot_cols = 2 * kGrid * tile_columns(n_req, n_tok, G);
+  char* w = static_cast<char*>(work);
+  a.meta = reinterpret_cast<int4*>(w);
+  w += round256(kGrid * (int64_t)sizeof(int4));
+  a.part_ml = reinterpret_cast<float2*>(w);
+  w += round256(slot_cols * 8);
+  a.part_o = reinterpret_cast<float*>(w);
+  w += round256(slot_cols * d * 4);
   if (cache && n_sel > 0) {
     if (q_stride != (int64_t)n_q_heads * d)
       return pages_fail(MILO_ERR_UNSUPPORTED, "with a cache the rows of q must follow one another (stride %lld)",
                         (long long)q_stride);
     const int64_t cols = (int64_t)n_tok * n_q_heads;
-    float2* ml = static_cast<float2*>(work);
-    float* o = reinterpret_cast<float*>(static_cast<char*>(work) + round256(cols * 8));
+    float2* ml = reinterpret_cast<float2*>(w);
+    float* o = reinterpret_cast<float*>(w + round256(cols * 8));
     int e = MILO_ERR_OUT_OF_MEMORY;
     try {
       e = attend_context(cache, block_table, n_sel, n_tok, n_q_heads, q, scale, o, ml, hip_stream);
@@ -189,15 +639,11 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   a.lg_page = log2_page(pages->page_tokens);
   a.causal = causal;
   a.out_bf16 = out_format == MILO_OUT_BF16;
-  const dim3 grid(n_tok, n_q_heads);
-  const bool e4m3 = pages->format == MILO_KV_E4M3;
-  if (d == 64) {
-    if (e4m3) hipLaunchKernelGGL((pages_simple_kernel<64, MILO_KV_E4M3>), grid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((pages_simple_kernel<64, MILO_KV_INT8>), grid, dim3(64), 0, s, a);
-  } else {
-    if (e4m3) hipLaunchKernelGGL((pages_simple_kernel<128, MILO_KV_E4M3>), grid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((pages_simple_kernel<128, MILO_KV_INT8>), grid, dim3(64), 0, s, a);
-  }
+  const int tt = tile_columns(n_req, n_tok, G) / G;
+  a.min_rows = 256;
+  a.min_wgs = (int)std::min<int64_t>(kGrid, (int64_t)H * std::max((n_tok + tt - 1) / tt, std::min(n_req, n_tok)));
+  if (d == 64) launch_pages<64>(a, few, s);
+  else launch_pages<128>(a, few, s);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? MILO_OK : pages_fail(MILO_ERR_HIP, "attention kernel: %s", hipGetErrorString(e));
 }

@@ -131,7 +131,7 @@ def lib() -> ctypes.CDLL:
         L.milo_pages_store.restype = ctypes.c_int
         L.milo_pages_load.argtypes = [pp, vp, i32, vp, i64, vp, i64, vp]
         L.milo_pages_load.restype = ctypes.c_int
-        L.milo_attend_pages_work.argtypes = [i32, i32, i32, ctypes.c_int]
+        L.milo_attend_pages_work.argtypes = [i32, i32, i32, i32, i32, ctypes.c_int]
         L.milo_attend_pages_work.restype = i64
         L.milo_attend_pages.argtypes = [vp, _c_i32p, i32, pp, vp, i32, vp, vp, i32, vp, i64, i32, i32, i32,
                                         ctypes.c_float, vp, i32, vp, vp]
@@ -625,7 +625,7 @@ def milo_attend_pages(pages: MiloPages, page_table, lens, q, scale: float, out, 
             raise ValueError("block_table without a cache")
     elif cache not in _CACHES:
         raise ValueError("unknown cache handle (not created by milo_cache_create, or already freed)")
-    need = lib().milo_attend_pages_work(n_tok, h_q, p.head_dim, 1 if n_sel else 0)
+    need = lib().milo_attend_pages_work(n_req, n_tok, h_q, p.n_kv_heads, p.head_dim, 1 if n_sel else 0)
     if work is None:
         with _on_stream(stream):
             work = torch.empty(need, dtype=torch.uint8, device=q.device)

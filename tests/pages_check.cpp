@@ -1,0 +1,112 @@
+// Checks the division of a paged attention call's work into shares (milo_pages.h) on the
+// host: over random batches every tile's rows are covered once, in order, by consecutive
+// shares, and the shares agree on who holds what.  Prints "ok <calls> <tiles> <split tiles>".
+#include <cstdio>
+#include <cstdlib>
+#include <random>
+#include <vector>
+
+#include "milo_pages.h"
+
+namespace milo {
+int report_error(int code, const char*) { return code; }
+}
+using namespace milo;
+
+#define CHECK(c)                                                       \
+  do {                                                                 \
+    if (!(c)) {                                                        \
+      std::printf("line %d: %s (call %d)\n", __LINE__, #c, call);      \
+      return 1;                                                        \
+    }                                                                  \
+  } while (0)
+
+int main() {
+  std::mt19937 rng(11);
+  auto pick = [&](int lo, int hi) { return lo + (int)(rng() % (unsigned)(hi - lo + 1)); };
+  long tiles_seen = 0, split = 0;
+  int call = 0;
+  for (; call < 3000; ++call) {
+    const int n_req = pick(1, call % 3 ? 6 : 400), H = pick(1, 8), tt = pick(1, 256), causal = pick(0, 1);
+    const int long_n = call % 5 == 0 ? 100000 : 700, many = call % 4 == 0 ? 900 : 5;
+    std::vector<Request> req(n_req);
+    int start = 0;
+    for (auto& q : req) {
+      q.m = pick(0, 3) ? pick(0, many) : pick(0, 1);
+      q.n = pick(0, 3) ? pick(0, long_n) : pick(0, 2) * 64;
+      q.start = start;
+      start += q.m;
+    }
+    int calls_out = 0;
+    const auto get = [&](int r) {
+      if (r < 0 || r >= n_req) {
+        ++calls_out;
+        return Request{0, 1, 0};
+      }
+      return req[r];
+    };
+    std::vector<int64_t> pre(n_req + 1, 0);
+    for (int r = 0; r < n_req; ++r) {
+      const int all = (req[r].m + tt - 1) / tt;
+      int64_t sum = 0;
+      for (int k = 0; k < all; ++k) {
+        CHECK(tiles_cost(req[r], k, tt, causal) == sum);
+        sum += kTileCost + seen_upto(req[r], (k + 1) * tt, causal);
+      }
+      CHECK(request_cost(req[r], tt, causal) == sum);
+      pre[r + 1] = pre[r] + H * sum;
+    }
+    const int64_t X = pre[n_req];
+    if (X == 0) continue;
+    const int W = (int)std::min<int64_t>(pick(1, 512), X);
+    // the tiles in order, each with the row up to which it is done
+    int r = 0, head = 0, tile = 0, done = 0, parts = 0, last_end = -1;
+    while (req[r].m == 0) ++r;
+    for (int w = 0; w < W; ++w) {
+      const int64_t b0 = share_begin(w, X, W), b1 = share_begin(w + 1, X, W);
+      CHECK(b0 < b1);
+      int lo = 0;
+      while (pre[lo + 1] <= b0) ++lo;
+      lo = lo > 2 ? lo - pick(0, 2) : lo;  // any request before will do
+      Place at = place_of(get, lo, pre[lo], b0, H, tt, causal);
+      bool first = true;
+      for (int64_t pos = b0; pos < b1;) {
+        CHECK(calls_out == 0 && at.r == r && at.head == head && at.tile == tile);
+        const Request q = at.rq;
+        const int j0 = tile * tt, ntok = std::min(tt, q.m - j0), vis = seen_upto(q, j0 + ntok, causal);
+        CHECK(ntok >= 1 && vis <= q.n);
+        const int64_t p0 = at.p, p1 = p0 + kTileCost + vis;
+        CHECK(p0 <= pos && pos < p1 && (first || p0 == pos));
+        const int ra = row_at(b0, p0, p1, vis), rb = row_at(b1, p0, p1, vis);
+        CHECK(ra == done && ra <= rb && rb <= vis && (ra % kRowAlign == 0 || ra == vis));
+        CHECK(share_holding(pos, X, W) == w && share_holding(std::min(p1, b1) - 1, X, W) == w);
+        const bool whole = b0 <= p0 && b1 >= p1;
+        CHECK(!whole || (ra == 0 && rb == vis && parts == 0));
+        if (!whole && b0 <= p0) last_end = share_holding(p1 - 1, X, W);
+        if (!whole) CHECK(parts == 0 ? b0 <= p0 && b1 < p1 : first);
+        done = rb;
+        ++parts;
+        pos = p1;
+        if (b1 >= p1) {  // the tile ends here
+          CHECK(done == vis && (whole || last_end == w));
+          ++tiles_seen;
+          split += parts > 1;
+          done = parts = 0;
+          if (++tile >= (req[r].m + tt - 1) / tt) {
+            tile = 0;
+            if (++head >= H) {
+              head = 0;
+              do ++r;
+              while (r < n_req && req[r].m == 0);
+            }
+          }
+        }
+        first = false;
+        if (pos < b1) next_tile(get, at, p1, H, tt);
+      }
+    }
+    CHECK(r == n_req && calls_out == 0);
+  }
+  std::printf("ok %d %ld %ld\n", call, tiles_seen, split);
+  return 0;
+}

@@ -5,8 +5,8 @@ element by element, from the roundings on the way (u = 2^-24 that of fp32, size 
 of |values| under the softmax, reach = the largest sum |q_c k_c| scale of a score):
  - a score is a sum of d exact products and three roundings more: (d + 8) u reach, which a
    weight takes on as a relative error;
- - a weight enters the value product as one bf16 (2^-8) or as two (2^-16), and 2^-22 covers
-   the exponential;
+ - a weight enters the value product as one bf16 (2^-8) for bf16 output, whole for fp32 output,
+   and 2^-22 covers the exponential;
  - sums of up to n weights or weighted values, and their rescalings: (n / 8 + 64) u;
  - the output's own rounding, 2^-8 of it as bf16."""
 import numpy as np
@@ -284,7 +284,7 @@ class Batch:
     def check(self, got, want):
         out, size, reach = want
         n, d = max(int(self.lens.max()), 1), out.shape[-1]
-        lost = 2.0 ** -8 if got.dtype == torch.bfloat16 else 2.0 ** -16
+        lost = 2.0 ** -8 if got.dtype == torch.bfloat16 else 0.0
         rel = (d + 8) * U * reach[..., None] + 2.0 ** -22 + (n / 8 + 64) * U
         tol = (2 * rel + lost) * size + (2.0 ** -8 * np.abs(out) if got.dtype == torch.bfloat16 else 0) + 1e-30
         err = np.abs(f64(got) - out)
@@ -469,7 +469,7 @@ def test_a_serving_loop(fmt):
         if bufs is None:
             bufs = dict(x=x, delta=i32(delta), out=torch.empty((n, H_q, d), device="cuda"), starts=i32([0] * (n_req + 1)),
                         slots=i32([0] * n), status=i32([0]),
-                        work=torch.empty(milo.lib().milo_attend_pages_work(n, H_q, d, 0), dtype=torch.uint8, device="cuda"),
+                        work=torch.empty(milo.lib().milo_attend_pages_work(n_req, n, H_q, H, d, 0), dtype=torch.uint8, device="cuda"),
                         plan=torch.empty(milo.lib().milo_pages_plan_work(n_req) // 4, dtype=torch.int32, device="cuda"))
         else:
             bufs["x"].copy_(x)
