@@ -463,8 +463,9 @@ int milo_pages_load(const milo_pages* pages, const int32_t* slots, int32_t n_tok
  *   work         milo_attend_pages_work bytes, 256-byte aligned: this call's alone until
  *                its work has run.
  * Scores, softmax sums and outputs are accumulated in fp32 from the exact codes; the
- * weights enter the value product in bf16 for bf16 output, in three bf16 parts (all of
- * their 24 bits) for fp32 output.
+ * weights enter the value product in fp16 (2^-11) for bf16 output, in two fp16 parts
+ * (2^-22) for fp32 output, or to 2^-32 of the row that adds most.  Values of a page and
+ * head whose scale is below 2^-96 count as zeros.
  * Errors: INVALID_ARG, UNSUPPORTED, and with a cache those of milo_attend_decode. */
 #define MILO_OUT_F32 0
 #define MILO_OUT_BF16 1

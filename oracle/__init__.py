@@ -514,12 +514,12 @@ def pages_plan(lens, delta, page_tokens: int, table, ring, head: int, count: int
 
 def attend_pages(keys, values, q, scale: float, causal: bool):
     """One request's queries q [m][H_q][d] over its rows keys / values [n][H_kv][d] in fp64; query j
-    sees the first n - m + j + 1 rows when causal.  Returns (out, size, reach): size = the same
-    average of |values|, reach [m][H_q] = the largest sum |q_c k_c| scale of a score (both for
-    error bounds).  A query that sees nothing gets zeros."""
+    sees the first n - m + j + 1 rows when causal.  Returns (out, size, reach, peak), the last three for error
+    bounds: size = the same average of |values|, reach [m][H_q] = the largest sum |q_c k_c| scale of
+    a score, peak [m][H_q] = the largest weight.  A query that sees nothing gets zeros."""
     n, m, G = keys.shape[0], q.shape[0], q.shape[1] // keys.shape[1]
     out, size = np.zeros(q.shape), np.zeros(q.shape)
-    reach = np.zeros(q.shape[:2])
+    reach, peak = np.zeros(q.shape[:2]), np.zeros(q.shape[:2])
     for h in range(q.shape[1]):
         K, V = keys[:, h // G], values[:, h // G]
         s_all = (q[:, h] @ K.T) * scale
@@ -531,5 +531,5 @@ def attend_pages(keys, values, q, scale: float, causal: bool):
             w = np.exp(s_all[j, :c] - s_all[j, :c].max())
             out[j, h] = w @ V[:c] / w.sum()
             size[j, h] = w @ np.abs(V[:c]) / w.sum()
-            reach[j, h] = r_all[j, :c].max()
-    return out, size, reach
+            reach[j, h], peak[j, h] = r_all[j, :c].max(), w.max() / w.sum()
+    return out, size, reach, peak

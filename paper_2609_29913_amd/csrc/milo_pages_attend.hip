@@ -35,6 +35,8 @@ __device__ inline int start_of(const PagesArgs& a, int i) {
 
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -62,11 +64,39 @@ __device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi) {
   return v;
 }
 
+// eight codes as fp16, exactly.  INT8: with the sign bit turned, byte u = code + 128
+// under the high byte 0x64 is the fp16 value 1024 + u.
+template <int FMT>
+__device__ __forceinline__ f16x8 codes_f16(uint32_t lo, uint32_t hi) {
+  f16x2 x[4];
+  if constexpr (FMT == MILO_KV_INT8) {
+    const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
+    lo ^= 0x80808080u;
+    hi ^= 0x80808080u;
+    x[0] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u)) - off;
+    x[1] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u)) - off;
+    x[2] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u)) - off;
+    x[3] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)) - off;
+  } else {
+    x[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false);
+    x[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true);
+    x[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false);
+    x[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
+  }
+  return f16x8{x[0][0], x[0][1], x[1][0], x[1][1], x[2][0], x[2][1], x[3][0], x[3][1]};
+}
+
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
+__device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
 __device__ __forceinline__ int lane_of(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
 __device__ __forceinline__ float lane_of(float v, int l) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l));
@@ -109,11 +139,17 @@ __device__ inline void finish(const PagesArgs& a, int64_t col, int d, int D, flo
 }
 
 // Pages of one request as a wave reads them: lane i holds the id and scales of page
-// base + i, so a step takes them without waiting for memory.
+// base + i, so a step takes them without waiting for memory.  The values' scale stands
+// as its logarithm, which joins the score (see add_step), and as its reciprocal; a
+// page of less than 2^-96 (none at all, as a rule) adds no values: it counts with the least
+// of the other scales, and its reciprocal is negative.
 struct Window {
   int base, id;
-  float ks, vs;
+  float ks;        // scale of the keys, times the call's, in log2 units
+  float lv, rv;    // log2 of the values' scale, 1 / scale
 };
+constexpr float kMinValueScale = 1.262177448e-29f;  // 2^-96
+__device__ __forceinline__ bool no_values(float rv) { return __float_as_int(rv) < 0; }
 
 __device__ inline Window window_at(const PagesArgs& a, int req, int head, int base, int last_page) {
   Window w;
@@ -124,8 +160,21 @@ __device__ inline Window window_at(const PagesArgs& a, int req, int head, int ba
   w.id = in ? id : 0;
   const int64_t at = (int64_t)w.id * a.p.n_kv_heads + head;
   const float nan = __uint_as_float(0x7FC00000u);
-  w.ks = in ? a.p.k_scale[at] : nan;
-  w.vs = in ? a.p.v_scale[at] : nan;
+  const float vs = a.p.v_scale[at];
+  w.ks = in ? a.p.k_scale[at] * a.qscale : nan;
+  w.lv = __builtin_amdgcn_logf(vs);
+  w.rv = vs == vs ? exp2_hw(-w.lv) : 1.f;
+  const bool none = vs < kMinValueScale;
+  if (__any(none)) {
+    float least = none || vs != vs ? INFINITY : w.lv;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) least = fminf(least, __shfl_xor(least, o));
+    if (least == INFINITY) least = 0.f;
+    if (none) {
+      w.lv = least;
+      w.rv = -exp2_hw(-least);
+    }
+  }
   return w;
 }
 
@@ -133,7 +182,8 @@ __device__ inline Window window_at(const PagesArgs& a, int req, int head, int ba
 template <int D, int GS>
 struct Step {
   uint4 k[GS][D / 64], v[GS][D / 64];
-  float ks[GS], vs[GS];
+  float ks[GS], lv[GS], rv[GS];
+  bool plain;  // every page adds values
 };
 
 template <int D, int GS>
@@ -142,12 +192,15 @@ __device__ __forceinline__ void load_step(const PagesArgs& a, int req, int head,
   const int P = 1 << a.lg_page, lane = threadIdx.x & 63;
   if ((row >> a.lg_page) - w.base >= 64) w = window_at(a, req, head, row >> a.lg_page, last_page);
   const int64_t head_bytes = (int64_t)P * D, page_bytes = head_bytes * a.p.n_kv_heads;
+  st.plain = true;
 #pragma unroll
   for (int g = 0; g < GS; ++g) {
     const int r = row + 16 * g, pg = min(r >> a.lg_page, last_page), li = min(pg - w.base, 63);
     const int id = lane_of(w.id, li);
     st.ks[g] = lane_of(w.ks, li);
-    st.vs[g] = lane_of(w.vs, li);
+    st.lv[g] = lane_of(w.lv, li);
+    st.rv[g] = lane_of(w.rv, li);
+    st.plain &= !no_values(st.rv[g]);
     const int64_t at = id * page_bytes + head * head_bytes + (r & (P - 1)) * D;
     const uint8_t* kp = static_cast<const uint8_t*>(a.p.k_codes) + at;
     const uint8_t* vp = static_cast<const uint8_t*>(a.p.v_codes) + at;
@@ -160,7 +213,8 @@ __device__ __forceinline__ void load_step(const PagesArgs& a, int req, int head,
 }
 
 // A wave's running softmax over NT tiles of 16 columns: lane (n = l % 16, q = l / 16)
-// holds of column n the maximum (all four q alike), its own part of the sum, and dims
+// holds of column n the exponent m that sums are relative to (all four q alike, -inf
+// before any row), its own part of the sum, and dims
 // 16 t + 4 q .. + 3 of the outputs.
 template <int D, int NT>
 struct Running {
@@ -171,11 +225,14 @@ struct Running {
 // Adds a step's rows.  Scores: 16x16x32 products keys x queries, so lane (n, q) holds
 // rows 4 q .. 4 q + 3 of each group for column n; two groups' weights are, as they
 // stand, the right operand of the product with the values' 32 rows in the order the
-// codes are stored in.  The reference that weights are taken relative to moves only
-// when a score passes it by 2^8, which fp32 sums bear.
-template <int D, int FMT, int PARTS, int NT, int GS>
-__device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&qf)[NT][D / 32], float qscale, int row,
-                                         int n, const int (&vis)[NT], bool masked, Running<D, NT>& run) {
+// codes are stored in.  A row's weight is taken with its values' scale, 2^(s + log2 v),
+// to 2^m, m at first 7 below the largest such exponent: fp16 then holds it with 2^-11
+// (2^-22 in two parts) of itself or, if it is less than 2^-21 of the largest, with 2^-32 of
+// that, whatever the pages' scales; the sum takes the scale out again.  m moves only when
+// a weight passes 2^15, which fp16 still holds.
+template <bool MASKED, int D, int FMT, int PARTS, int NT, int GS>
+__device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&qf)[NT][D / 32], int row,
+                                         int n, const int (&vis)[NT], Running<D, NT>& run) {
   const int lane = threadIdx.x & 63, q4 = (lane >> 4) * 4;
   f32x4 s[GS][NT];
 #pragma unroll
@@ -190,14 +247,17 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
 #pragma unroll
       for (int t = 0; t < NT; ++t) s[g][t] = mfma16(a1, qf[t][2 * j + 1], s[g][t]);
     }
+    __builtin_amdgcn_sched_barrier(0);
   }
+  // the conversions of the phases stay in them: moved up, they cost registers (spills)
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int g = 0; g < GS; ++g)
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[g][t][i] *= st.ks[g] * qscale;
-  if (masked) {
+      for (int i = 0; i < 4; ++i) s[g][t][i] = fmaf(s[g][t][i], st.ks[g], st.lv[g]);
+  if constexpr (MASKED) {
 #pragma unroll
     for (int g = 0; g < GS; ++g)
 #pragma unroll
@@ -213,10 +273,10 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
     for (int g = 0; g < GS; ++g)
 #pragma unroll
       for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[g][t][i]);
-    if (__any(mx > run.m[t] + 8.f)) {
+    if (__any(mx > run.m[t] + 15.f)) {
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       mx = fmaxf(mx, __shfl_xor(mx, 32));
-      mx = fmaxf(mx, run.m[t]);
+      mx = fmaxf(mx - 7.f, run.m[t]);
       const float f = mx == -INFINITY ? 1.f : exp2_hw(run.m[t] - mx);
       run.m[t] = mx;
       run.l[t] *= f;
@@ -224,40 +284,34 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
       for (int c = 0; c < D / 16; ++c) run.o[t][c] *= f;
     }
   }
-  bf16x8 w[GS / 2][NT][PARTS];
+  f16x8 w[GS / 2][NT][PARTS];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const float ref = run.m[t] == -INFINITY ? 0.f : run.m[t];
-    float sum = 0.f;
 #pragma unroll
-    for (int g = 0; g < GS; ++g)
+    for (int g = 0; g < GS; ++g) {
+      float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float x = exp2_hw(s[g][t][i] - ref);
-        sum += x;
-        x *= st.vs[g];
-        // a page of NaN that a column does not see must not reach it
-        if (masked && row + 16 * g + q4 + i >= vis[t]) x = 0.f;
         const int e = (g & 1) * 4 + i;
-        if constexpr (PARTS == 1) {
-          w[g / 2][t][0][e] = (__bf16)x;  // 2^-9
-        } else {  // three bf16 hold all 24 bits
-          const float h = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u), r = x - h;
-          const float h2 = __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
-          w[g / 2][t][0][e] = (__bf16)h;
-          w[g / 2][t][1][e] = (__bf16)h2;
-          w[g / 2][t][2][e] = (__bf16)(r - h2);
-        }
+        sum += x;
+        if (MASKED && no_values(st.rv[g])) x = 0.f;
+        w[g / 2][t][0][e] = (_Float16)x;
+        if constexpr (PARTS == 2) w[g / 2][t][1][e] = (_Float16)(x - (float)w[g / 2][t][0][e]);
       }
-    run.l[t] += sum;
+      run.l[t] = fmaf(sum, MASKED ? fabsf(st.rv[g]) : st.rv[g], run.l[t]);
+    }
   }
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int g = 0; g < GS; g += 2) {
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
+      __builtin_amdgcn_sched_barrier(0);
       uint32_t va[4] = {st.v[g][j].x, st.v[g][j].y, st.v[g][j].z, st.v[g][j].w};
       uint32_t vb[4] = {st.v[g + 1][j].x, st.v[g + 1][j].y, st.v[g + 1][j].z, st.v[g + 1][j].w};
-      if (FMT == MILO_KV_E4M3 && masked) {  // rows behind the request's last hold anything, NaN among it
+      if constexpr (FMT == MILO_KV_E4M3 && MASKED) {  // rows behind the request's last hold anything, NaN among it
         const int na = min(max(n - row - 16 * g - q4, 0), 4), nb = min(max(n - row - 16 * g - 16 - q4, 0), 4);
         const uint32_t ka = na == 4 ? ~0u : (1u << 8 * na) - 1u, kb = nb == 4 ? ~0u : (1u << 8 * nb) - 1u;
 #pragma unroll
@@ -268,7 +322,7 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
       }
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const bf16x8 vf = codes_bf16<FMT>(va[c], vb[c]);
+        const f16x8 vf = codes_f16<FMT>(va[c], vb[c]);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -314,7 +368,7 @@ __global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(Pag
     pre[1 + tid] = before + inc;
     __syncthreads();
   }
-  const int64_t X = H * pre[kPagesThreads];
+  const int64_t X = uniform(H * pre[kPagesThreads]);
   // (a share is at least kTileCost long, so none is empty)
   int W = (int)min(min((int64_t)gridDim.x, X / kTileCost), max(X / a.min_rows, (int64_t)a.min_wgs));
   if (W >= kXcds) W -= W % kXcds;
@@ -323,7 +377,7 @@ __global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(Pag
   if ((int)blockIdx.x >= W || X == 0) return;
   // consecutive shares on one XCD, whose L2 then holds the rows that tiles share
   const int w = W >= kXcds ? (int)(blockIdx.x % kXcds) * (W / kXcds) + blockIdx.x / kXcds : blockIdx.x;
-  const int64_t b0 = share_begin(w, X, W), b1 = share_begin(w + 1, X, W);
+  const int64_t b0 = uniform(share_begin(w, X, W)), b1 = uniform(share_begin(w + 1, X, W));
 
   // the tile that b0 falls in
   Place at;
@@ -336,6 +390,8 @@ __global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(Pag
       else hi = mid;
     }
     at = place_of(get, lo * chunk, H * pre[lo], b0, H, tt, a.causal);
+    at = Place{uniform(at.r), uniform(at.head), uniform(at.tile), uniform(at.p),
+               Request{uniform(at.rq.start), uniform(at.rq.m), uniform(at.rq.n)}};
   }
   bool first = true;
   int parity = 0;
@@ -343,7 +399,7 @@ __global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(Pag
     const int j0 = uniform(at.tile * tt), ntok = uniform(min(tt, at.rq.m - at.tile * tt)), n = uniform(at.rq.n);
     const int req = uniform(at.r), g = uniform(at.head), start = uniform(at.rq.start), m = uniform(at.rq.m);
     const int vis_hi = uniform(seen_upto(at.rq, j0 + ntok, a.causal));
-    const int64_t p0 = at.p, p1 = p0 + kTileCost + vis_hi;
+    const int64_t p0 = uniform(at.p), p1 = p0 + kTileCost + vis_hi;
     const int ra = uniform(row_at(b0, p0, p1, vis_hi)), rb = uniform(row_at(b1, p0, p1, vis_hi));
     const bool whole = b0 <= p0 && b1 >= p1;
     const int slot = 2 * w + (first ? 0 : 1);
@@ -392,13 +448,22 @@ __global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(Pag
       Window win = window_at(a, req, g, wa >> a.lg_page, last_page);
       Step<D, GS> s0, s1;
       load_step(a, req, g, win, wa, last_page, s0);
-      for (int row = wa;;) {
+      int row = wa;
+      for (; row + 2 * ROWS <= min(vis_lo, wb) && s0.plain; row += 2 * ROWS) {
+        load_step(a, req, g, win, row + ROWS, last_page, s1);
+        add_step<false, D, FMT, PARTS, NT, GS>(s0, qf, row, n, vis, run);
+        if (!s1.plain) {
+          s0 = s1;
+          row += ROWS;
+          break;
+        }
+        if (row + 2 * ROWS < wb) load_step(a, req, g, win, row + 2 * ROWS, last_page, s0);
+        add_step<false, D, FMT, PARTS, NT, GS>(s1, qf, row + ROWS, n, vis, run);
+      }
+      for (; row < wb; row += ROWS) {  // the last ones, whose rows not every column sees
         if (row + ROWS < wb) load_step(a, req, g, win, row + ROWS, last_page, s1);
-        add_step<D, FMT, PARTS, NT, GS>(s0, qf, a.qscale, row, n, vis, row + ROWS > vis_lo, run);
-        if ((row += ROWS) >= wb) break;
-        if (row + ROWS < wb) load_step(a, req, g, win, row + ROWS, last_page, s0);
-        add_step<D, FMT, PARTS, NT, GS>(s1, qf, a.qscale, row, n, vis, row + ROWS > vis_lo, run);
-        if ((row += ROWS) >= wb) break;
+        add_step<true, D, FMT, PARTS, NT, GS>(s0, qf, row, n, vis, run);
+        if (row + ROWS < wb) s0 = s1;
       }
     }
 #pragma unroll
@@ -483,32 +548,57 @@ __global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(Pag
 }
 
 // Joins the parts of the tile that begins in share w and ends in share we: its own
-// slot and the first slot of the shares after it, in this order.
+// slot and the first slot of the shares after it.  A workgroup takes a column at a
+// time; its lanes of D / 4 threads take every PL-th part in turn, four at once, and
+// are joined in order.
 template <int D, int COLS>
 __global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) {
-  constexpr int TPC = D / 4;  // threads of a column
+  constexpr int TPC = D / 4, PL = kPagesThreads / TPC, U = 4;
+  __shared__ float2 lane_ml[PL];
+  __shared__ float4 lane_o[PL][TPC];
   const int4 mt = a.meta[blockIdx.x];
   if (mt.x < 0) return;
-  const int s0 = mt.z, we = mt.w, w = s0 >> 1;
-  for (int x = blockIdx.y * kPagesThreads + threadIdx.x; x < mt.y * TPC; x += gridDim.y * kPagesThreads) {
-    const int c = x / TPC, d = x % TPC * 4;
-    float m = -INFINITY, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = w; k <= we; ++k) {
-      const int64_t at = (int64_t)(k == w ? s0 : 2 * k) * COLS + c;
-      const float2 ml = a.part_ml[at];
-      const float4 y = *reinterpret_cast<const float4*>(a.part_o + at * D + d);
-      if (ml.x == -INFINITY && ml.y == 0.f) continue;
-      const float mx = fmaxf(m, ml.x);
-      const float f = m == -INFINITY ? 1.f : exp2_hw(m - mx), fy = ml.x == -INFINITY ? 1.f : exp2_hw(ml.x - mx);
-      l = l * f + ml.y * fy;
-      o.x = o.x * f + y.x * fy;
-      o.y = o.y * f + y.y * fy;
-      o.z = o.z * f + y.z * fy;
-      o.w = o.w * f + y.w * fy;
-      m = mx;
+  const int s0 = mt.z, we = mt.w, w = s0 >> 1, dq = threadIdx.x % TPC, pl = threadIdx.x / TPC;
+  float m, l;
+  float4 o;
+  const auto add = [&](float2 ml, const float4& y) {
+    if (ml.x == -INFINITY && ml.y == 0.f) return;  // a part without rows
+    const float mx = fmaxf(m, ml.x);
+    const float f = m == -INFINITY ? 1.f : exp2_hw(m - mx), fy = ml.x == -INFINITY ? 1.f : exp2_hw(ml.x - mx);
+    l = l * f + ml.y * fy;
+    o.x = o.x * f + y.x * fy;
+    o.y = o.y * f + y.y * fy;
+    o.z = o.z * f + y.z * fy;
+    o.w = o.w * f + y.w * fy;
+    m = mx;
+  };
+  for (int c = blockIdx.y; c < mt.y; c += gridDim.y) {
+    m = -INFINITY;
+    l = 0.f;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = w + pl; k0 <= we; k0 += PL * U) {
+      float2 ml[U];
+      float4 y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = min(k0 + u * PL, we);
+        const int64_t at = (int64_t)(k == w ? s0 : 2 * k) * COLS + c;
+        ml[u] = a.part_ml[at];
+        y[u] = *reinterpret_cast<const float4*>(a.part_o + at * D + 4 * dq);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (k0 + u * PL <= we) add(ml[u], y[u]);
     }
-    finish(a, mt.x + (int64_t)(c / a.G) * a.H_q + c % a.G, d, D, m, l, o);
+    if (dq == 0) lane_ml[pl] = make_float2(m, l);
+    lane_o[pl][dq] = o;
+    __syncthreads();
+    if (pl == 0) {
+#pragma unroll
+      for (int k = 1; k < PL; ++k) add(lane_ml[k], lane_o[k][dq]);
+      finish(a, mt.x + (int64_t)(c / a.G) * a.H_q + c % a.G, 4 * dq, D, m, l, o);
+    }
+    __syncthreads();
   }
 }
 
@@ -525,7 +615,7 @@ template <int D, int FMT, int PARTS>
 void launch_pages(const PagesArgs& a, bool few, hipStream_t s) {
   if (few) {
     hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 1, true>), dim3(kGrid), dim3(kPagesThreads), 0, s, a);
-    hipLaunchKernelGGL((pages_join_kernel<D, 16>), dim3(kGrid, 2), dim3(kPagesThreads), 0, s, a);
+    hipLaunchKernelGGL((pages_join_kernel<D, 16>), dim3(kGrid, 8), dim3(kPagesThreads), 0, s, a);
   } else {
     hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 4, false>), dim3(kGrid), dim3(kPagesThreads), 0, s, a);
     hipLaunchKernelGGL((pages_join_kernel<D, 256>), dim3(kGrid, 16), dim3(kPagesThreads), 0, s, a);
@@ -539,8 +629,8 @@ void launch_pages(const PagesArgs& a, bool few, hipStream_t s) {
     if (e4m3) launch_pages<D, MILO_KV_E4M3, 1>(a, few, s);
     else launch_pages<D, MILO_KV_INT8, 1>(a, few, s);
   } else {
-    if (e4m3) launch_pages<D, MILO_KV_E4M3, 3>(a, few, s);
-    else launch_pages<D, MILO_KV_INT8, 3>(a, few, s);
+    if (e4m3) launch_pages<D, MILO_KV_E4M3, 2>(a, few, s);
+    else launch_pages<D, MILO_KV_INT8, 2>(a, few, s);
   }
 }
 

@@ -5,8 +5,9 @@ element by element, from the roundings on the way (u = 2^-24 that of fp32, size 
 of |values| under the softmax, reach = the largest sum |q_c k_c| scale of a score):
  - a score is a sum of d exact products and three roundings more: (d + 8) u reach, which a
    weight takes on as a relative error;
- - a weight enters the value product as one bf16 (2^-8) for bf16 output, whole for fp32 output,
-   and 2^-22 covers the exponential;
+ - a weight enters the value product as one fp16 (2^-11) for bf16 output, as two (2^-22) for
+   fp32 output, or, small, off by 2^-32 of the largest (each of n rows of codes up to 448, under
+   the largest scale, for the largest weight peak); 2^-22 covers the exponential;
  - sums of up to n weights or weighted values, and their rescalings: (n / 8 + 64) u;
  - the output's own rounding, 2^-8 of it as bf16."""
 import numpy as np
@@ -273,7 +274,7 @@ class Batch:
     def want(self, causal):
         parts = [oracle.attend_pages(*self.kv(i), f64(self.q[self.starts[i]:self.starts[i + 1]]), self.scale, causal)
                  for i in range(len(self.lens))]
-        return [np.concatenate([p[k] for p in parts]) for k in range(3)]
+        return [np.concatenate([p[k] for p in parts]) for k in range(4)]
 
     def run(self, causal=True, dtype=torch.float32, **kw):
         out = torch.full(self.q.shape, float("nan"), dtype=dtype, device="cuda")
@@ -282,11 +283,12 @@ class Batch:
         return out
 
     def check(self, got, want):
-        out, size, reach = want
+        out, size, reach, peak = want
         n, d = max(int(self.lens.max()), 1), out.shape[-1]
-        lost = 2.0 ** -8 if got.dtype == torch.bfloat16 else 0.0
+        lost = 2.0 ** -11 if got.dtype == torch.bfloat16 else 2.0 ** -22
+        small = n * 2.0 ** -32 * 448 * np.nanmax(self.scales[1]) * peak[..., None]
         rel = (d + 8) * U * reach[..., None] + 2.0 ** -22 + (n / 8 + 64) * U
-        tol = (2 * rel + lost) * size + (2.0 ** -8 * np.abs(out) if got.dtype == torch.bfloat16 else 0) + 1e-30
+        tol = (2 * rel + lost) * size + small + (2.0 ** -8 * np.abs(out) if got.dtype == torch.bfloat16 else 0) + 1e-30
         err = np.abs(f64(got) - out)
         assert np.all(np.isfinite(f64(got))) and np.all(err <= tol), float(np.max(err / tol))
 
@@ -335,6 +337,42 @@ def test_attend_long(lens, counts):
     got = b.run()
     b.check(got, b.want(True))
     assert torch.equal(got, b.run())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attend_values_of_very_different_scales(dtype):
+    """Pages whose values lie 2^40 apart, pages of zeros, requests of each kind alone: what small
+    pages hold is not lost to the large ones' requests beside them."""
+    b = Batch(21, [64, 100, 16, 400, 48], [1, 2, 1, 3, 1], HEADS["0.5b"], 16, "int8")
+    for i, (lo, hi) in enumerate([(-70, -70), (-20, 20), (0, 0), (-4, 14), (-60, 30)]):
+        for j, pg in enumerate(b.table[i, :-(-b.lens[i] // 16)]):
+            b.scales[1][pg] = 0.0 if i == 2 or j == 1 else np.float32(2.0) ** (lo if j % 2 else hi)
+    put(b.pages, *b.rows, *b.scales)
+    b.lens = np.asarray(b.lens)
+    want = b.want(True)
+    got = b.run(True, dtype)
+    whole = b.scales[1].copy()
+    for i in range(5):  # each request against the scales of its own pages
+        at = slice(b.starts[i], b.starts[i + 1])
+        b.scales[1] = whole[b.table[i, :-(-b.lens[i] // 16)]]
+        b.check(got[at], [w[at] for w in want])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attend_a_row_that_takes_the_weight_and_adds_nothing(dtype):
+    """One row with nearly all of the weight and values of zero before thousands that share the
+    rest: what is left of the output is theirs, to the usual error."""
+    b = Batch(22, [9000, 500], [1, 1], HEADS["one"], 16, "int8")
+    for i in range(2):
+        first = b.table[i, 0]
+        b.rows[0][first, 0], b.rows[1][first, 0] = 0, 0
+        q = f64(b.q[i, 0])
+        b.rows[0][first, 0, 0] = np.rint(127 * q / np.abs(q).max())
+        b.scales[0][first] = np.float32((np.log(2e5) + 5) / (b.scale * (q @ b.rows[0][first, 0, 0])))
+    put(b.pages, *b.rows, *b.scales)
+    want = b.want(True)
+    assert want[3].min() > 0.9
+    b.check(b.run(True, dtype), want)
 
 
 def test_attend_many_requests():

@@ -52,7 +52,7 @@ def test_store_grows_a_page_and_starts_it_afresh():
 def test_attention_is_torch_attention(causal):
     rng = np.random.default_rng(5)
     k, v, q = rng.standard_normal((23, 2, 64)), rng.standard_normal((23, 2, 64)), rng.standard_normal((7, 6, 64))
-    out, size, _ = oracle.attend_pages(k, v, q, 0.3, causal)
+    out, size, _, _ = oracle.attend_pages(k, v, q, 0.3, causal)
     mask = torch.ones(7, 23, dtype=torch.bool).tril(16) if causal else torch.ones(7, 23, dtype=torch.bool)
     rep = lambda x: torch.from_numpy(x).transpose(0, 1).repeat_interleave(3, 0)  # noqa: E731
     want = torch.nn.functional.scaled_dot_product_attention(torch.from_numpy(q).transpose(0, 1), rep(k), rep(v),
@@ -61,7 +61,7 @@ def test_attention_is_torch_attention(causal):
 
 
 def test_a_query_before_every_row_gets_zeros():
-    out, _, _ = oracle.attend_pages(np.ones((2, 1, 64)), np.ones((2, 1, 64)), np.ones((4, 1, 64)), 1.0, True)
+    out, _, _, _ = oracle.attend_pages(np.ones((2, 1, 64)), np.ones((2, 1, 64)), np.ones((4, 1, 64)), 1.0, True)
     assert np.all(out[:2] == 0) and np.all(out[2:] == 1)
 
 
