@@ -26,6 +26,7 @@ struct PagesArgs {
   float qscale;            // scale * log2(e)
   int32_t min_rows;        // positions a workgroup gets at least,
   int32_t min_wgs;         // unless fewer workgroups than this would work
+  int32_t whole_tiles;     // 1: a workgroup takes one whole tile, no shares
   int32_t n_req, n_tok, H_q, G, width, lg_page, causal, out_bf16;
 };
 
@@ -251,49 +252,47 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
   }
   // the conversions of the phases stay in them: moved up, they cost registers (spills)
   __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-  for (int g = 0; g < GS; ++g)
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[g][t][i] = fmaf(s[g][t][i], st.ks[g], st.lv[g]);
-  if constexpr (MASKED) {
-#pragma unroll
-    for (int g = 0; g < GS; ++g)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (row + 16 * g + q4 + i >= vis[t]) s[g][t][i] = -INFINITY;
-  }
+  // exponents of the weights, relative to m (0 before any row)
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    float mx = s[0][t][0];
+    const float m0 = run.m[t] == -INFINITY ? 0.f : run.m[t];
+    float mx = -INFINITY;
 #pragma unroll
-    for (int g = 0; g < GS; ++g)
+    for (int g = 0; g < GS; ++g) {
+      const float base = st.lv[g] - m0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[g][t][i]);
-    if (__any(mx > run.m[t] + 15.f)) {
+      for (int i = 0; i < 4; ++i) {
+        float x = fmaf(s[g][t][i], st.ks[g], base);
+        if (MASKED && row + 16 * g + q4 + i >= vis[t]) x = -INFINITY;
+        s[g][t][i] = x;
+        mx = fmaxf(mx, x);
+      }
+    }
+    if (__any(mx > (run.m[t] == -INFINITY ? -INFINITY : 15.f))) {
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       mx = fmaxf(mx, __shfl_xor(mx, 32));
-      mx = fmaxf(mx - 7.f, run.m[t]);
-      const float f = mx == -INFINITY ? 1.f : exp2_hw(run.m[t] - mx);
-      run.m[t] = mx;
+      // up by what the largest passes 2^7 (from none: there, up or down)
+      const float up = mx == -INFINITY ? 0.f : run.m[t] == -INFINITY ? mx - 7.f : fmaxf(mx - 7.f, 0.f);
+      const float f = run.m[t] == -INFINITY ? 0.f : exp2_hw(-up);
+      if (mx != -INFINITY) run.m[t] = m0 + up;
       run.l[t] *= f;
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) run.o[t][c] *= f;
+#pragma unroll
+      for (int g = 0; g < GS; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[g][t][i] -= up;
     }
   }
   f16x8 w[GS / 2][NT][PARTS];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const float ref = run.m[t] == -INFINITY ? 0.f : run.m[t];
 #pragma unroll
     for (int g = 0; g < GS; ++g) {
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float x = exp2_hw(s[g][t][i] - ref);
+        float x = exp2_hw(s[g][t][i]);
         const int e = (g & 1) * 4 + i;
         sum += x;
         if (MASKED && no_values(st.rv[g])) x = 0.f;
@@ -335,8 +334,8 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
 // SHARE: the workgroup's waves split a tile's rows (16 NT columns), else its columns
 // (64 NT columns, every wave reads all rows).
 template <int D, int FMT, int PARTS, int NT, bool SHARE>
-__global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(PagesArgs a) {
-  constexpr int GS = NT == 1 ? 4 : 2, ROWS = 16 * GS;
+__global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
+  constexpr int GS = SHARE ? 4 : 2, ROWS = 16 * GS;
   constexpr int COLS = SHARE ? 16 * NT : 16 * NT * kPagesWaves;
   constexpr int OS = D + 4;  // row stride of a column's partial in LDS
   __shared__ int64_t pre[kPagesThreads + 1];
@@ -351,7 +350,8 @@ __global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(Pag
   {
     int64_t own = 0;
     for (int r = tid * chunk; r < min((tid + 1) * chunk, a.n_req); ++r) {
-      own += request_cost(request_of(a, r), tt, a.causal);
+      const Request q = request_of(a, r);
+      own += a.whole_tiles ? (q.m + tt - 1) / tt : request_cost(q, tt, a.causal);
     }
     int64_t inc = own;
 #pragma unroll
@@ -370,14 +370,18 @@ __global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(Pag
   }
   const int64_t X = uniform(H * pre[kPagesThreads]);
   // (a share is at least kTileCost long, so none is empty)
+  if (a.whole_tiles && blockIdx.x >= X) return;
   int W = (int)min(min((int64_t)gridDim.x, X / kTileCost), max(X / a.min_rows, (int64_t)a.min_wgs));
   if (W >= kXcds) W -= W % kXcds;
   int4* meta = a.meta + blockIdx.x;
-  if (tid == 0) *meta = make_int4(-1, 0, 0, 0);
-  if ((int)blockIdx.x >= W || X == 0) return;
+  if (!a.whole_tiles) {
+    if (tid == 0) *meta = make_int4(-1, 0, 0, 0);
+    if ((int)blockIdx.x >= W || X == 0) return;
+  }
   // consecutive shares on one XCD, whose L2 then holds the rows that tiles share
   const int w = W >= kXcds ? (int)(blockIdx.x % kXcds) * (W / kXcds) + blockIdx.x / kXcds : blockIdx.x;
-  const int64_t b0 = uniform(share_begin(w, X, W)), b1 = uniform(share_begin(w + 1, X, W));
+  int64_t b0 = uniform(share_begin(w, X, W)), b1 = uniform(share_begin(w + 1, X, W));
+  if (a.whole_tiles) b0 = blockIdx.x;
 
   // the tile that b0 falls in
   Place at;
@@ -389,9 +393,25 @@ __global__ __launch_bounds__(kPagesThreads, SHARE ? 2 : 1) void pages_kernel(Pag
       if (H * pre[mid] <= b0) lo = mid;
       else hi = mid;
     }
-    at = place_of(get, lo * chunk, H * pre[lo], b0, H, tt, a.causal);
+    if (!a.whole_tiles) {
+      at = place_of(get, lo * chunk, H * pre[lo], b0, H, tt, a.causal);
+    } else {  // a request's last tiles, which see most, first; its heads side by side
+      int x = (int)(b0 - H * pre[lo]), n_tiles;
+      for (at.r = lo * chunk;; ++at.r) {
+        at.rq = request_of(a, at.r);
+        n_tiles = (at.rq.m + tt - 1) / tt;
+        if (x < H * n_tiles) break;
+        x -= H * n_tiles;
+      }
+      at.head = x % H;
+      at.tile = n_tiles - 1 - x / H;
+      at.p = b0 = 0;
+      b1 = kTileCost + seen_upto(at.rq, (at.tile + 1) * tt, a.causal);
+    }
     at = Place{uniform(at.r), uniform(at.head), uniform(at.tile), uniform(at.p),
                Request{uniform(at.rq.start), uniform(at.rq.m), uniform(at.rq.n)}};
+    b0 = uniform(b0);
+    b1 = uniform(b1);
   }
   bool first = true;
   int parity = 0;
@@ -604,34 +624,38 @@ __global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) 
 
 int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
 
-constexpr int kGrid = 512;  // workgroups at most: two on every CU
+constexpr int kGrid = 512;  // workgroups that share the work: two on every CU
 
-// Columns of a workgroup's tile: 16 where requests bring few queries each (the waves
-// split the rows), else 256 (the waves split the columns).
-bool few_columns(int32_t n_req, int32_t n_tok, int G) { return (int64_t)n_tok * G <= 32 * (int64_t)n_req; }
-int tile_columns(int32_t n_req, int32_t n_tok, int G) { return few_columns(n_req, n_tok, G) ? 16 : 64 * kPagesWaves; }
+// How a call's columns are tiled: 16 to a workgroup whose waves split the rows where
+// requests bring few queries each, else 64 or 128 whose waves split the columns.
+enum Tiling { kFew, kSome, kMany };
+Tiling tiling_of(int32_t n_req, int32_t n_tok, int G) {
+  const int64_t cols = (int64_t)n_tok * G;
+  return cols <= 24 * (int64_t)n_req ? kFew : cols <= 64 * (int64_t)n_req ? kSome : kMany;
+}
+int tile_columns(Tiling t) { return t == kFew ? 16 : t == kSome ? 64 : 128; }
 
 template <int D, int FMT, int PARTS>
-void launch_pages(const PagesArgs& a, bool few, hipStream_t s) {
-  if (few) {
-    hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 1, true>), dim3(kGrid), dim3(kPagesThreads), 0, s, a);
-    hipLaunchKernelGGL((pages_join_kernel<D, 16>), dim3(kGrid, 8), dim3(kPagesThreads), 0, s, a);
-  } else {
-    hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 4, false>), dim3(kGrid), dim3(kPagesThreads), 0, s, a);
-    hipLaunchKernelGGL((pages_join_kernel<D, 256>), dim3(kGrid, 16), dim3(kPagesThreads), 0, s, a);
-  }
+void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
+  if (t == kFew) hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 1, true>), dim3(grid), dim3(kPagesThreads), 0, s, a);
+  else if (t == kSome) hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 1, false>), dim3(grid), dim3(kPagesThreads), 0, s, a);
+  else hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 2, false>), dim3(grid), dim3(kPagesThreads), 0, s, a);
 }
 
 template <int D>
-void launch_pages(const PagesArgs& a, bool few, hipStream_t s) {
+void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
   const bool e4m3 = a.p.format == MILO_KV_E4M3;
   if (a.out_bf16) {
-    if (e4m3) launch_pages<D, MILO_KV_E4M3, 1>(a, few, s);
-    else launch_pages<D, MILO_KV_INT8, 1>(a, few, s);
+    if (e4m3) launch_pages<D, MILO_KV_E4M3, 1>(a, t, grid, s);
+    else launch_pages<D, MILO_KV_INT8, 1>(a, t, grid, s);
   } else {
-    if (e4m3) launch_pages<D, MILO_KV_E4M3, 2>(a, few, s);
-    else launch_pages<D, MILO_KV_INT8, 2>(a, few, s);
+    if (e4m3) launch_pages<D, MILO_KV_E4M3, 2>(a, t, grid, s);
+    else launch_pages<D, MILO_KV_INT8, 2>(a, t, grid, s);
   }
+  if (a.whole_tiles) return;
+  if (t == kFew) hipLaunchKernelGGL((pages_join_kernel<D, 16>), dim3(kGrid, 8), dim3(kPagesThreads), 0, s, a);
+  else if (t == kSome) hipLaunchKernelGGL((pages_join_kernel<D, 64>), dim3(kGrid, 16), dim3(kPagesThreads), 0, s, a);
+  else hipLaunchKernelGGL((pages_join_kernel<D, 128>), dim3(kGrid, 16), dim3(kPagesThreads), 0, s, a);
 }
 
 }  // namespace
@@ -644,7 +668,7 @@ extern "C" {
 int64_t milo_attend_pages_work(int32_t n_req, int32_t n_tok, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                int with_cache) {
   if (n_req < 0 || n_tok < 0 || n_kv_heads < 1 || n_q_heads < n_kv_heads || head_dim < 1) return 0;
-  const int64_t cols = (int64_t)n_tok * n_q_heads, slot_cols = 2 * kGrid * tile_columns(n_req, n_tok, n_q_heads / n_kv_heads);
+  const int64_t cols = (int64_t)n_tok * n_q_heads, slot_cols = 2 * kGrid * tile_columns(tiling_of(n_req, n_tok, n_q_heads / n_kv_heads));
   int64_t bytes = round256(kGrid * (int64_t)sizeof(int4)) + round256(slot_cols * 8) + round256(slot_cols * head_dim * 4);
   if (with_cache) bytes += round256(cols * 8) + round256(cols * head_dim * 4);
   return bytes;
@@ -687,8 +711,8 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   if (!work || !aligned_to(work, 256)) return pages_fail(MILO_ERR_INVALID_ARG, "work must be non-NULL and 256-byte aligned");
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   PagesArgs a{};
-  const bool few = few_columns(n_req, n_tok, G);
-  const int64_t slot_cols = 2 * kGrid * tile_columns(n_req, n_tok, G);
+  const Tiling tiling = tiling_of(n_req, n_tok, G);
+  const int64_t slot_cols = 2 * kGrid * tile_columns(tiling);
   char* w = static_cast<char*>(work);
   a.meta = reinterpret_cast<int4*>(w);
   w += round256(kGrid * (int64_t)sizeof(int4));
@@ -729,11 +753,16 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   a.lg_page = log2_page(pages->page_tokens);
   a.causal = causal;
   a.out_bf16 = out_format == MILO_OUT_BF16;
-  const int tt = tile_columns(n_req, n_tok, G) / G;
+  // tiles at least (each request that has queries has one) and at most
+  const int tt = tile_columns(tiling) / G;
+  const int64_t least = (int64_t)H * std::max((n_tok + tt - 1) / tt, std::min(n_req, n_tok));
+  const int64_t most = (int64_t)H * (n_tok / tt + std::min(n_req, n_tok));
   a.min_rows = 256;
-  a.min_wgs = (int)std::min<int64_t>(kGrid, (int64_t)H * std::max((n_tok + tt - 1) / tt, std::min(n_req, n_tok)));
-  if (d == 64) launch_pages<64>(a, few, s);
-  else launch_pages<128>(a, few, s);
+  a.min_wgs = (int)std::min<int64_t>(kGrid, least);
+  a.whole_tiles = tiling != kFew && least >= kGrid / 2;
+  const int grid = a.whole_tiles ? (int)most : kGrid;
+  if (d == 64) launch_pages<64>(a, tiling, grid, s);
+  else launch_pages<128>(a, tiling, grid, s);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? MILO_OK : pages_fail(MILO_ERR_HIP, "attention kernel: %s", hipGetErrorString(e));
 }
