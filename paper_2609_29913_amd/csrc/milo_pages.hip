@@ -20,6 +20,7 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kFillThreads = 256;
 constexpr int kMaxPlanReq = 1 << 24;
+constexpr int kOneLaunch = 4096;  // new rows that one workgroup writes the slots of
 
 enum PlanStatus : int { kPoolShort = 1, kRowNarrow = 2, kBadLength = 4, kSlotsShort = 8, kBadRing = 16 };
 
@@ -61,7 +62,21 @@ __device__ inline Sums plan_one(const PlanArgs& a, int i, int* flags) {
   return {m > n ? m - n : 0, p1 > p0 ? p1 - p0 : 0, p0 > p1 ? p0 - p1 : 0};
 }
 
+// the slot of packed new row x, which is row `row` of request i, whose first `held` pages
+// are in the table and whose others are the ring's from the taken-th on
+__device__ inline int slot_at(const PlanArgs& a, int i, int row, int held, int taken, int head) {
+  const int pg = row >> a.lg_page, P = 1 << a.lg_page;
+  const int id = pg < held ? a.table[(int64_t)i * a.width + pg] : a.ring[((int64_t)head + taken + pg - held) % a.n_pages];
+  return (uint32_t)id < (uint32_t)a.n_pages ? (id << a.lg_page) + (row & (P - 1)) : -1;
+}
+
+__device__ inline int owner_of(const int32_t* first, int n, int x);
+
+// FILL: n_req <= kPlanThreads; the workgroup also writes slots and pages, the sums in
+// LDS, so that a decode step's plan is one launch.
+template <bool FILL>
 __global__ __launch_bounds__(kPlanThreads) void plan_scan_kernel(PlanArgs a) {
+  __shared__ int first[FILL ? 4 : 1][FILL ? kPlanThreads : 1];  // starts, taken, given, length before
   __shared__ Sums wave_sum[kPlanThreads / 64];
   __shared__ int all_flags;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -84,9 +99,18 @@ __global__ __launch_bounds__(kPlanThreads) void plan_scan_kernel(PlanArgs a) {
     for (int w = 0; w < kPlanThreads / 64; ++w) carry = add(carry, wave_sum[w]);
     if (i < a.n_req) {
       // sums past 2^31 are cut: such a step is stopped below and they are not used
-      a.starts[i] = (int32_t)(before.rows + inc.rows - own.rows);
-      a.taken[i] = (int32_t)(before.taken + inc.taken - own.taken);
-      a.given[i] = (int32_t)(before.given + inc.given - own.given);
+      const Sums at{before.rows + inc.rows - own.rows, before.taken + inc.taken - own.taken,
+                    before.given + inc.given - own.given};
+      a.starts[i] = (int32_t)at.rows;
+      if constexpr (FILL) {
+        first[0][i] = (int32_t)at.rows;
+        first[1][i] = (int32_t)at.taken;
+        first[2][i] = (int32_t)at.given;
+        first[3][i] = a.lens[i];
+      } else {
+        a.taken[i] = (int32_t)at.taken;
+        a.given[i] = (int32_t)at.given;
+      }
     }
   }
   __syncthreads();
@@ -107,12 +131,34 @@ __global__ __launch_bounds__(kPlanThreads) void plan_scan_kernel(PlanArgs a) {
     a.ring_state_out[0] = (int32_t)(flags ? head : (head + carry.taken) % n);
     a.ring_state_out[1] = (int32_t)(flags ? count : count - carry.taken + carry.given);
     a.status[0] = flags;
-    a.total[0] = flags ? 0 : (int32_t)carry.taken;
-    a.total[1] = flags ? 0 : (int32_t)carry.given;
-    a.total[2] = flags;
-    a.total[3] = (int32_t)head;
-    a.total[4] = (int32_t)count;
-    a.total[5] = flags ? 0 : (int32_t)carry.rows;
+    if constexpr (!FILL) {
+      a.total[0] = flags ? 0 : (int32_t)carry.taken;
+      a.total[1] = flags ? 0 : (int32_t)carry.given;
+      a.total[3] = (int32_t)head;
+      a.total[4] = (int32_t)count;
+      a.total[5] = flags ? 0 : (int32_t)carry.rows;
+    }
+  }
+  if constexpr (FILL) {
+    const int rows = flags ? 0 : (int)carry.rows, taken = flags ? 0 : (int)carry.taken, given = flags ? 0 : (int)carry.given;
+    const int P = 1 << a.lg_page, items = a.n_slots + taken + given;
+    for (int x = tid; x < items; x += kPlanThreads) {
+      if (x < a.n_slots) {
+        int slot = -1;
+        if (x < rows) {
+          const int i = owner_of(first[0], a.n_req, x), n = first[3][i];
+          slot = slot_at(a, i, n + x - first[0][i], (n + P - 1) >> a.lg_page, first[1][i], (int)head);
+        }
+        a.slots[x] = slot;
+      } else if (x < a.n_slots + taken) {
+        const int y = x - a.n_slots, i = owner_of(first[1], a.n_req, y), held = (first[3][i] + P - 1) >> a.lg_page;
+        a.table[(int64_t)i * a.width + held + y - first[1][i]] = a.ring[(head + y) % a.n_pages];
+      } else {
+        const int y = x - a.n_slots - taken, i = owner_of(first[2], a.n_req, y);
+        const int kept = (first[3][i] + a.delta[i] + P - 1) >> a.lg_page;
+        a.ring[(head + count + y) % a.n_pages] = a.table[(int64_t)i * a.width + kept + y - first[2][i]];
+      }
+    }
   }
 }
 
@@ -137,10 +183,7 @@ __global__ __launch_bounds__(kFillThreads) void plan_fill_kernel(PlanArgs a) {
       if (x < rows) {
         const int i = owner_of(a.starts, a.n_req, (int)x);
         const int n = a.lens_out[i] - a.delta[i];  // length before (delta > 0 here)
-        const int row = n + (int)x - a.starts[i], pg = row >> a.lg_page, held = (n + P - 1) >> a.lg_page;
-        const int id = pg < held ? a.table[(int64_t)i * a.width + pg]
-                                 : a.ring[((int64_t)head + a.taken[i] + pg - held) % a.n_pages];
-        if ((uint32_t)id < (uint32_t)a.n_pages) slot = (id << a.lg_page) + (row & (P - 1));
+        slot = slot_at(a, i, n + (int)x - a.starts[i], (n + P - 1) >> a.lg_page, a.taken[i], head);
       }
       a.slots[x] = slot;
     } else if (x < (int64_t)a.n_slots + taken) {
@@ -156,8 +199,11 @@ __global__ __launch_bounds__(kFillThreads) void plan_fill_kernel(PlanArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Store.  One wave per (row, KV head): the row that begins a page's run of new
-// rows does the whole run of that page, the others leave at once.
+// Store and load.  A wave takes a page's (or 16 output rows') part of one KV head and
+// side at a time, in groups of 16 rows: lane (q, ch) has rows 4 q .. 4 q + 3 and dims
+// 8 ch .. 8 ch + 7, four 16-byte accesses on the bf16 side; on the codes' side 8 bytes
+// of keys per row, or per dim the dword of a value's four rows.  With 64 dims a wave
+// holds two groups.
 // ---------------------------------------------------------------------------
 constexpr int kRowThreads = 256;
 
@@ -168,6 +214,7 @@ struct StoreArgs {
   int64_t k_stride, v_stride;
   const int32_t* slots;
   int32_t n_tok, lg_page, n_slots;
+  int32_t chunk;  // rows of the call a wave looks at
 };
 
 __device__ inline uint32_t wave_max(uint32_t x) {
@@ -176,54 +223,152 @@ __device__ inline uint32_t wave_max(uint32_t x) {
   return x;
 }
 
-// keys (VALUES false) or values of rows t0 .. t0 + run - 1 into offsets off .. of
-// a page and head
+__device__ inline uint32_t abs_max2(uint32_t m, uint32_t x) {  // both halves
+  const uint32_t lo = max(m & 0xFFFFu, x & 0x7FFFu), hi = max(m >> 16, (x >> 16) & 0x7FFFu);
+  return lo | hi << 16;
+}
+
+// eight bf16 values (16 bytes) under scale s as eight codes; E4M3 scales are powers
+// of two, whose reciprocal is exact
+template <int FMT>
+__device__ __forceinline__ uint2 codes_of_row(const uint4& x, float s) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = bf16_value(w[i] & 0xFFFFu);
+    f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+  if (!(s > 0.f)) return make_uint2(0, 0);
+  if constexpr (FMT == MILO_KV_E4M3) {
+    const float r = 1.f / s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] *= r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __fdiv_rn(f[i], s);
+  }
+  return make_uint2(codes_of<FMT>(make_float4(f[0], f[1], f[2], f[3])), codes_of<FMT>(make_float4(f[4], f[5], f[6], f[7])));
+}
+
+// the four codes of a dword under scale `was`, under scale s
+template <int FMT>
+__device__ __forceinline__ uint32_t rescaled(uint32_t w, float was, float s) {
+  const float4 c = code_values<FMT>(w);
+  return codes_of<FMT>(over<FMT>(make_float4(__fmul_rn(c.x, was), __fmul_rn(c.y, was), __fmul_rn(c.z, was),
+                                             __fmul_rn(c.w, was)), s));
+}
+
+// byte b of words a, b, c, d as one word
+__device__ __forceinline__ uint32_t gather_byte(uint32_t a, uint32_t b, uint32_t c, uint32_t d, int k) {
+  const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0C0C0000u | (uint32_t)(4 + k) << 8 | (uint32_t)k);
+  const uint32_t hi = __builtin_amdgcn_perm(d, c, 0x0C0C0000u | (uint32_t)(4 + k) << 8 | (uint32_t)k);
+  return lo | hi << 16;
+}
+
+// rows x .. (run of them) into offsets off .. of a page and head: keys (VALUES false)
+// or values
 template <int D, int FMT, bool VALUES>
 __device__ void store_side(const uint16_t* x, int64_t stride, uint8_t* codes, float* scale_at, int off, int run) {
-  const int lane = threadIdx.x & 63;
-  uint32_t amax = 0;
-  for (int i = lane; i < run * D; i += 64) amax = max(amax, (uint32_t)x[(int64_t)(i / D) * stride + i % D] & 0x7FFFu);
-  amax = wave_max(amax);
-  const float was = *scale_at;
-  float s = scale_of<FMT>(amax);
-  if (off > 0 && !(s >= was)) s = was >= s || was != was ? was : s;  // the larger, NaN before all
-  if (off > 0 && s != was && s == s) {  // rows that are held, under the larger scale
-    for (int i = lane; i < off * D; i += 64) {
-      const int b = VALUES ? value_byte(i / D, i % D, D) : key_byte(i / D, i % D, D);
-      const float c = code_values<FMT>(codes[b]).x;
-      codes[b] = (uint8_t)codes_of<FMT>(over<FMT>(make_float4(__fmul_rn(c, was), 0.f, 0.f, 0.f), s));
+  constexpr int LPG = D / 2, GPW = 64 / LPG;  // lanes of a group of 16 rows, groups of a wave
+  const int lane = threadIdx.x & 63, sub = lane / LPG, ch = lane % (D / 8), q = lane % LPG / (D / 8);
+  const float was = off > 0 ? *scale_at : 0.f;
+  const int g0 = off >> 4, g1 = (off + run + 15) >> 4;
+  uint4 v[4];
+  const auto load = [&](int g) {  // the group's new rows, zeros in the others
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = 16 * g + 4 * q + i - off;
+      v[i] = t >= 0 && t < run ? *reinterpret_cast<const uint4*>(x + (int64_t)t * stride + 8 * ch) : make_uint4(0, 0, 0, 0);
     }
+  };
+  uint32_t mx = 0;
+  for (int g = g0 + sub; g < g1; g += GPW) {
+    load(g);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx = abs_max2(abs_max2(abs_max2(abs_max2(mx, v[i].x), v[i].y), v[i].z), v[i].w);
   }
-  for (int i = lane; i < run * D; i += 64) {
-    const int t = off + i / D, c = i % D;
-    const float f = bf16_value(x[(int64_t)(i / D) * stride + c]);
-    codes[VALUES ? value_byte(t, c, D) : key_byte(t, c, D)] = (uint8_t)codes_of<FMT>(over<FMT>(make_float4(f, 0.f, 0.f, 0.f), s));
+  float s = scale_of<FMT>(wave_max(max(mx & 0xFFFFu, mx >> 16)));
+  if (off > 0 && !(s >= was)) s = was >= s || was != was ? was : s;  // the larger, NaN before all
+  const bool grew = off > 0 && s != was && s == s;
+  const bool loaded = g1 - g0 <= GPW;  // the new rows are still in registers
+  for (int g = (grew ? 0 : g0) + sub; g < g1; g += GPW) {
+    if (g >= g0 && !(loaded && g - sub == g0)) load(g);
+    uint2 c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = codes_of_row<FMT>(v[i], s);
+    const int t0 = 16 * g + 4 * q;
+    if constexpr (!VALUES) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = t0 + i;
+        uint2* at = reinterpret_cast<uint2*>(codes + key_byte(t, 8 * ch, D));
+        if (t >= off) {
+          if (t < off + run) *at = c[i];
+        } else if (grew) {
+          const uint2 w = *at;
+          *at = make_uint2(rescaled<FMT>(w.x, was, s), rescaled<FMT>(w.y, was, s));
+        }
+      }
+    } else {
+      // which of the quad's rows are new and which held
+      uint32_t fresh = 0, held = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int t = t0 + i;
+        if (t >= off && t < off + run) fresh |= 255u << 8 * i;
+        if (t < off) held |= 255u << 8 * i;
+      }
+      if (fresh || (held && grew)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          uint32_t w = e < 4 ? gather_byte(c[0].x, c[1].x, c[2].x, c[3].x, e) : gather_byte(c[0].y, c[1].y, c[2].y, c[3].y, e - 4);
+          uint32_t* at = reinterpret_cast<uint32_t*>(codes + value_byte(t0, 8 * ch + e, D));
+          if (fresh != ~0u) {
+            const uint32_t old = *at;
+            w = (w & fresh) | (old & ~fresh);
+            if (grew) w = (w & ~held) | (rescaled<FMT>(old, was, s) & held);
+          }
+          *at = w;
+        }
+      }
+    }
   }
   if (lane == 0) *scale_at = s;
 }
 
+// Waves: `chunk` rows of the call by 2 H (head, side) pairs.  A row that begins a run
+// (rows that follow one another in a page) does it whole; the others are passed over.
 template <int D, int FMT>
 __global__ __launch_bounds__(kRowThreads) void store_kernel(StoreArgs a) {
-  const int H = a.p.n_kv_heads;
-  const int64_t item = (int64_t)blockIdx.x * (kRowThreads / 64) + (threadIdx.x >> 6);
-  const int t = (int)(item / H), h = (int)(item % H);
-  if (t >= a.n_tok) return;
-  const int slot = a.slots[t], P = 1 << a.lg_page;
-  if ((uint32_t)slot >= (uint32_t)a.n_slots) return;
-  const int off = slot & (P - 1), page = slot >> a.lg_page;
-  if (off > 0 && t > 0 && a.slots[t - 1] == slot - 1) return;  // inside another row's run
-  int run = 1;
-  while (run < P - off && t + run < a.n_tok && a.slots[t + run] == slot + run) ++run;
-  const int64_t ph = (int64_t)page * H + h;
-  store_side<D, FMT, false>(a.k + (int64_t)t * a.k_stride + h * D, a.k_stride, (uint8_t*)a.p.k_codes + ph * P * D,
-                            a.p.k_scale + ph, off, run);
-  store_side<D, FMT, true>(a.v + (int64_t)t * a.v_stride + h * D, a.v_stride, (uint8_t*)a.p.v_codes + ph * P * D,
-                           a.p.v_scale + ph, off, run);
+  const int H = a.p.n_kv_heads, P = 1 << a.lg_page, lane = threadIdx.x & 63;
+  const int pair = blockIdx.y * (kRowThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (pair >= 2 * H) return;
+  const int h = pair >> 1;
+  const int64_t t1 = min((int64_t)a.n_tok, ((int64_t)blockIdx.x + 1) * a.chunk);
+  for (int64_t t = (int64_t)blockIdx.x * a.chunk; t < t1; ++t) {
+    const int slot = __builtin_amdgcn_readfirstlane(a.slots[t]);
+    if ((uint32_t)slot >= (uint32_t)a.n_slots) continue;
+    const int off = slot & (P - 1);
+    if (off > 0 && t > 0 && a.slots[t - 1] == slot - 1) continue;
+    int run = 0;  // rows whose slots go on from this one's in the page
+    for (int k = 0; k < P; k += 64) {
+      const int r = k + lane;
+      const bool on = r < P - off && t + r < a.n_tok && a.slots[t + r] == slot + r;
+      const uint64_t m = __ballot(on);
+      run += ~m == 0 ? 64 : __builtin_ctzll(~m);
+      if (~m != 0) break;
+    }
+    const int64_t ph = (int64_t)(slot >> a.lg_page) * H + h;
+    if (pair & 1)
+      store_side<D, FMT, true>(a.v + t * a.v_stride + h * D, a.v_stride, (uint8_t*)a.p.v_codes + ph * P * D,
+                               a.p.v_scale + ph, off, run);
+    else
+      store_side<D, FMT, false>(a.k + t * a.k_stride + h * D, a.k_stride, (uint8_t*)a.p.k_codes + ph * P * D,
+                                a.p.k_scale + ph, off, run);
+  }
 }
 
-// ---------------------------------------------------------------------------
-// Load.  One wave per (row, KV head).
-// ---------------------------------------------------------------------------
 struct LoadArgs {
   milo_pages p;
   uint16_t* k;
@@ -233,29 +378,90 @@ struct LoadArgs {
   int32_t n_tok, lg_page, n_slots;
 };
 
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) { return bf16_bits(a) | bf16_bits(b) << 16; }
+
+// Waves: 16 output rows (32 with 64 dims) by (head, side) pairs.  Rows may come from
+// anywhere; where a lane's four follow one another, as a request's do, their values
+// are in one or two dwords per dim.
 template <int D, int FMT>
 __global__ __launch_bounds__(kRowThreads) void load_kernel(LoadArgs a) {
-  const int lane = threadIdx.x & 63, H = a.p.n_kv_heads;
-  const int64_t item = (int64_t)blockIdx.x * (kRowThreads / 64) + (threadIdx.x >> 6);
-  const int t = (int)(item / H), h = (int)(item % H);
-  if (t >= a.n_tok) return;
-  const int slot = a.slots[t], P = 1 << a.lg_page;
-  const bool in = (uint32_t)slot < (uint32_t)a.n_slots;
-  const int64_t ph = in ? (int64_t)(slot >> a.lg_page) * H + h : 0;
-  const uint8_t* kc = (const uint8_t*)a.p.k_codes + ph * P * D;
-  const uint8_t* vc = (const uint8_t*)a.p.v_codes + ph * P * D;
-  for (int c = lane; c < D; c += 64) {
-    if (a.k) {
-      const float x = in ? a.p.k_scale[ph] * code_values<FMT>(kc[key_byte(slot & (P - 1), c, D)]).x : 0.f;
-      a.k[(int64_t)t * a.k_stride + h * D + c] = (uint16_t)bf16_bits(x);
+  constexpr int LPG = D / 2, GPW = 64 / LPG;
+  const int H = a.p.n_kv_heads, P = 1 << a.lg_page, lane = threadIdx.x & 63;
+  const int pair = blockIdx.y * (kRowThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (pair >= 2 * H) return;
+  const int h = pair >> 1;
+  const bool values = pair & 1;
+  uint16_t* out = values ? a.v : a.k;
+  if (!out) return;
+  const int64_t stride = values ? a.v_stride : a.k_stride;
+  const uint8_t* codes = static_cast<const uint8_t*>(values ? a.p.v_codes : a.p.k_codes);
+  const float* scales = values ? a.p.v_scale : a.p.k_scale;
+  const int ch = lane % (D / 8), q = lane % LPG / (D / 8);
+  const int64_t j0 = ((int64_t)blockIdx.x * GPW + lane / LPG) * 16 + 4 * q;
+  int slot[4];
+  float s[4];
+  const uint8_t* base[4];  // the row's page and head
+  bool in[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    slot[i] = j0 + i < a.n_tok ? a.slots[j0 + i] : -1;
+    in[i] = (uint32_t)slot[i] < (uint32_t)a.n_slots;
+    const int64_t ph = (int64_t)(in[i] ? slot[i] >> a.lg_page : 0) * H + h;
+    s[i] = scales[ph];
+    base[i] = codes + ph * P * D;
+    slot[i] = in[i] ? slot[i] & (P - 1) : 0;
+  }
+  uint2 c[4];  // the rows' eight codes
+  if (!values) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = *reinterpret_cast<const uint2*>(base[i] + key_byte(slot[i], 8 * ch, D));
+  } else {
+    const uint8_t* at[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) at[i] = base[i] + value_byte(slot[i] & ~3, 8 * ch, D);
+    const bool one = at[0] == at[3] && at[1] == at[0] && at[2] == at[0];
+    const bool two = (at[1] == at[0] || at[1] == at[3]) && (at[2] == at[0] || at[2] == at[3]);
+    // dim 8 ch + e of the same rows lies e dwords of 16 bytes on (value_byte)
+    uint32_t w[4][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[0][e] = *reinterpret_cast<const uint32_t*>(at[0] + 16 * e);
+    if (one) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[1][e] = w[2][e] = w[3][e] = w[0][e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[3][e] = *reinterpret_cast<const uint32_t*>(at[3] + 16 * e);
+      if (two) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          w[1][e] = at[1] == at[0] ? w[0][e] : w[3][e];
+          w[2][e] = at[2] == at[0] ? w[0][e] : w[3][e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          w[1][e] = *reinterpret_cast<const uint32_t*>(at[1] + 16 * e);
+          w[2][e] = *reinterpret_cast<const uint32_t*>(at[2] + 16 * e);
+        }
+      }
     }
-    if (a.v) {
-      const float x = in ? a.p.v_scale[ph] * code_values<FMT>(vc[value_byte(slot & (P - 1), c, D)]).x : 0.f;
-      a.v[(int64_t)t * a.v_stride + h * D + c] = (uint16_t)bf16_bits(x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int sh = (slot[i] & 3) * 8;
+      c[i].x = (w[i][0] >> sh & 255u) | (w[i][1] >> sh & 255u) << 8 | (w[i][2] >> sh & 255u) << 16 | (w[i][3] >> sh & 255u) << 24;
+      c[i].y = (w[i][4] >> sh & 255u) | (w[i][5] >> sh & 255u) << 8 | (w[i][6] >> sh & 255u) << 16 | (w[i][7] >> sh & 255u) << 24;
     }
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (j0 + i >= a.n_tok) continue;
+    const float4 x = code_values<FMT>(c[i].x), y = code_values<FMT>(c[i].y);
+    uint4 r = make_uint4(bf16_pair(s[i] * x.x, s[i] * x.y), bf16_pair(s[i] * x.z, s[i] * x.w),
+                         bf16_pair(s[i] * y.x, s[i] * y.y), bf16_pair(s[i] * y.z, s[i] * y.w));
+    if (!in[i]) r = make_uint4(0, 0, 0, 0);
+    *reinterpret_cast<uint4*>(out + (j0 + i) * stride + h * D + 8 * ch) = r;
+  }
 }
-
 
 #define MILO_PAGES_DISPATCH(kernel, a, grid, threads, s)                                            \
   do {                                                                                              \
@@ -320,7 +526,11 @@ int milo_pages_plan(const int32_t* lens, const int32_t* delta, int32_t n_req, in
   a.n_pages = n_pages;
   a.n_slots = n_slots;
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-  hipLaunchKernelGGL(plan_scan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+  if (n_req <= kPlanThreads && n_slots <= kOneLaunch) {
+    hipLaunchKernelGGL(plan_scan_kernel<true>, dim3(1), dim3(kPlanThreads), 0, s, a);
+    return launched("plan kernel");
+  }
+  hipLaunchKernelGGL(plan_scan_kernel<false>, dim3(1), dim3(kPlanThreads), 0, s, a);
   if (const int e = launched("plan kernel"); e != MILO_OK) return e;
   const int64_t items = (int64_t)n_slots + n_slots / page_tokens + n_req;
   const int grid = (int)std::min<int64_t>(2048, items / kFillThreads + 1);
@@ -348,10 +558,12 @@ int milo_pages_store(const milo_pages* pages, const uint16_t* k, int64_t k_strid
   a.n_tok = n_tok;
   a.lg_page = log2_page(pages->page_tokens);
   a.n_slots = pages->n_pages * pages->page_tokens;
-  const int64_t waves = (int64_t)n_tok * pages->n_kv_heads, wgs = (waves + kRowThreads / 64 - 1) / (kRowThreads / 64);
-  if (wgs > INT32_MAX) return pages_fail(MILO_ERR_UNSUPPORTED, "too many rows");
+  // Few rows: a wave for each, since each may begin a run; many: a wave for 16 of them,
+  // most of which are inside another's run.
+  a.chunk = n_tok <= 2048 ? 1 : 16;
+  const dim3 grid((n_tok + a.chunk - 1) / a.chunk, (2 * pages->n_kv_heads + 3) / 4);
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-  MILO_PAGES_DISPATCH(store_kernel, a, dim3((uint32_t)wgs), kRowThreads, s);
+  MILO_PAGES_DISPATCH(store_kernel, a, grid, kRowThreads, s);
   return launched("store kernel");
 }
 
@@ -378,10 +590,10 @@ int milo_pages_load(const milo_pages* pages, const int32_t* slots, int32_t n_tok
   a.n_tok = n_tok;
   a.lg_page = log2_page(pages->page_tokens);
   a.n_slots = pages->n_pages * pages->page_tokens;
-  const int64_t waves = (int64_t)n_tok * pages->n_kv_heads, wgs = (waves + kRowThreads / 64 - 1) / (kRowThreads / 64);
-  if (wgs > INT32_MAX) return pages_fail(MILO_ERR_UNSUPPORTED, "too many rows");
+  const int rows = pages->head_dim == 64 ? 32 : 16;
+  const dim3 grid((uint32_t)(((int64_t)n_tok + rows - 1) / rows), (2 * pages->n_kv_heads + 3) / 4);
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-  MILO_PAGES_DISPATCH(load_kernel, a, dim3((uint32_t)wgs), kRowThreads, s);
+  MILO_PAGES_DISPATCH(load_kernel, a, grid, kRowThreads, s);
   return launched("load kernel");
 }
 

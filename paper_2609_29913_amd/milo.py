@@ -478,6 +478,9 @@ def milo_pages_create(n_pages: int, page_tokens: int, n_kv_heads: int, head_dim:
     return MiloPages(*codes, *scales, page_tokens)
 
 
+# These calls are made once or more per layer and step, so their checks are cheap: one
+# comparison per property, messages only where one fails.
+
 def _pages_arg(pages) -> MiloPages:
     import torch
     if not isinstance(pages, MiloPages):
@@ -487,28 +490,45 @@ def _pages_arg(pages) -> MiloPages:
     return pages
 
 
-def _i32_dev(x, name: str, shape=None):
-    """A contiguous int32 tensor on the current GPU, of the given shape (-1: any)."""
-    _dev_tensor(x, name, ("torch.int32",), None if shape is None else len(shape))
-    if shape is not None and any(w >= 0 and w != n for w, n in zip(shape, x.shape)):
-        raise ValueError(f"{name} has shape {tuple(x.shape)}, expected {tuple(shape)}")
+def _i32_dev(x, name: str, dev: int, *shape: int):
+    """A contiguous int32 tensor on GPU `dev` of the given shape (-1: any)."""
+    import torch
+    if not isinstance(x, torch.Tensor) or x.dtype is not torch.int32 or x.get_device() != dev or not x.is_contiguous():
+        _dev_tensor(x, name, ("torch.int32",))
+    got = x.shape
+    if len(got) != len(shape):
+        raise ValueError(f"{name} must have {len(shape)} dimensions, got shape {tuple(got)}")
+    for w, n in zip(shape, got):
+        if w != n and w >= 0:
+            raise ValueError(f"{name} has shape {tuple(got)}, expected {tuple(shape)}")
     return x
 
 
-def _row_stride(x, name: str, heads: int, d: int) -> int:
+def _row_stride(x, name: str, dev: int, heads: int, d: int) -> int:
     """Row stride (elements) of bf16 rows [n][heads][d] whose rows may lie apart."""
     import torch
-    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must be a tensor on the current GPU")
-    if str(x.dtype) not in _BF16_DTYPES:
+    if not isinstance(x, torch.Tensor) or x.get_device() != dev:
+        raise ValueError(f"{name} must be a tensor on the current GPU (cuda:{dev})")
+    if x.dtype is not torch.bfloat16 and str(x.dtype) not in _BF16_DTYPES:
         raise ValueError(f"{name} must have dtype {' or '.join(_BF16_DTYPES)}, got {x.dtype}")
-    if x.dim() != 3 or tuple(x.shape[1:]) != (heads, d):
-        raise ValueError(f"{name} must be [n][{heads}][{d}], got {tuple(x.shape)}")
-    if x.shape[0] == 0:
+    shape = x.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{name} must be [n][{heads}][{d}], got {tuple(shape)}")
+    if shape[0] == 0:
         return heads * d
-    if x.stride(2) != 1 or (heads > 1 and x.stride(1) != d):
+    row, head, one = x.stride()
+    if one != 1 or (heads > 1 and head != d):
         raise ValueError(f"{name}'s rows of [{heads}][{d}] must be contiguous (strides {x.stride()})")
-    return int(x.stride(0)) if x.shape[0] > 1 else heads * d
+    return row if shape[0] > 1 else heads * d
+
+
+def _stream_on(stream, dev: int) -> int:
+    """Handle of `stream` (None: the current one of GPU `dev`, by torch's short way where it has it)."""
+    import torch
+    if stream is None:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return raw(dev) if raw is not None else _stream(None)
+    return _stream(stream)
 
 
 def _on_stream(stream):
@@ -534,66 +554,71 @@ def milo_pages_plan(lens, delta, page_tokens: int, table, ring, ring_state, n_sl
     made here where not given; slots has n_slots entries.  work: int32 tensor of at least
     milo_pages_plan_work(n_req) bytes, or None."""
     import torch
-    n_req = int(lens.shape[0]) if isinstance(lens, torch.Tensor) and lens.dim() == 1 else -1
-    if n_req < 0:
+    if not isinstance(lens, torch.Tensor) or not lens.is_cuda or lens.dim() != 1:
         raise ValueError("lens must be an int32 GPU tensor [n_req]")
-    _i32_dev(lens, "lens", (n_req,))
-    _i32_dev(delta, "delta", (n_req,))
-    _i32_dev(table, "table", (n_req, -1))
-    _i32_dev(ring, "ring", (-1,))
-    _i32_dev(ring_state, "ring_state", (2,))
-    if slots is None:
-        if n_slots is None:
-            raise ValueError("give slots, or n_slots for a new one")
-    elif n_slots is not None and n_slots != slots.shape[0]:
-        raise ValueError(f"slots has {slots.shape[0]} entries, n_slots is {n_slots}")
-    with _on_stream(stream):
-        def made(x, name, n):
-            return torch.empty(n, dtype=torch.int32, device=lens.device) if x is None else _i32_dev(x, name, (n,))
-        lens_out = made(lens_out, "lens_out", n_req)
-        ring_state_out = made(ring_state_out, "ring_state_out", 2)
-        starts = made(starts, "starts", n_req + 1)
-        slots = made(slots, "slots", int(n_slots) if slots is None else -1)
-        status = made(status, "status", 1)
-        need = lib().milo_pages_plan_work(n_req)
-        if work is None:
-            work = torch.empty(need // 4, dtype=torch.int32, device=lens.device)
-    if _i32_dev(work, "work").numel() * 4 < need:
+    n_req, dev = lens.shape[0], torch.cuda.current_device()
+    _i32_dev(lens, "lens", dev, n_req)
+    _i32_dev(delta, "delta", dev, n_req)
+    _i32_dev(table, "table", dev, n_req, -1)
+    _i32_dev(ring, "ring", dev, -1)
+    _i32_dev(ring_state, "ring_state", dev, 2)
+    if slots is not None:
+        _i32_dev(slots, "slots", dev, -1 if n_slots is None else n_slots)
+    elif n_slots is None:
+        raise ValueError("give slots, or n_slots for a new one")
+    need = lib().milo_pages_plan_work(n_req)
+    if work is not None and _i32_dev(work, "work", dev, -1).numel() * 4 < need:
         raise ValueError(f"work holds {work.numel() * 4} bytes, {need} are needed")
+    for name, x, n in (("lens_out", lens_out, n_req), ("ring_state_out", ring_state_out, 2), ("starts", starts, n_req + 1),
+                       ("status", status, 1)):
+        if x is not None:
+            _i32_dev(x, name, dev, n)
+    if lens_out is None or ring_state_out is None or starts is None or slots is None or status is None or work is None:
+        with _on_stream(stream):
+            def made(x, n):
+                return torch.empty(n, dtype=torch.int32, device=lens.device) if x is None else x
+            lens_out, ring_state_out, starts = made(lens_out, n_req), made(ring_state_out, 2), made(starts, n_req + 1)
+            slots, status, work = made(slots, n_slots), made(status, 1), made(work, need // 4)
     _check(lib().milo_pages_plan(
-        lens.data_ptr(), delta.data_ptr(), n_req, int(page_tokens), table.data_ptr(), int(table.shape[1]), ring.data_ptr(),
-        int(ring.shape[0]), ring_state.data_ptr(), ring_state_out.data_ptr(), lens_out.data_ptr(), starts.data_ptr(),
-        slots.data_ptr(), int(slots.shape[0]), status.data_ptr(), work.data_ptr(), _stream(stream)))
+        lens.data_ptr(), delta.data_ptr(), n_req, int(page_tokens), table.data_ptr(), table.shape[1], ring.data_ptr(),
+        ring.shape[0], ring_state.data_ptr(), ring_state_out.data_ptr(), lens_out.data_ptr(), starts.data_ptr(),
+        slots.data_ptr(), slots.shape[0], status.data_ptr(), work.data_ptr(), _stream_on(stream, dev)))
     return lens_out, starts, slots, ring_state_out, status
 
 
 def milo_pages_store(pages: MiloPages, k, v, slots, stream=None) -> None:
     """Quantise rows k, v (bf16 [n][H_kv][d]; rows may lie apart) into their slots (int32 [n])."""
     p = _pages_arg(pages)
-    ks, vs = _row_stride(k, "k", p.n_kv_heads, p.head_dim), _row_stride(v, "v", p.n_kv_heads, p.head_dim)
-    if v.shape[0] != k.shape[0]:
-        raise ValueError(f"k has {k.shape[0]} rows, v {v.shape[0]}")
-    _i32_dev(slots, "slots", (int(k.shape[0]),))
-    _check(lib().milo_pages_store(p._as_parameter_, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(), int(k.shape[0]),
-                                  _stream(stream)))
+    dev = p.device.index
+    ks, vs = _row_stride(k, "k", dev, p.n_kv_heads, p.head_dim), _row_stride(v, "v", dev, p.n_kv_heads, p.head_dim)
+    n = k.shape[0]
+    if v.shape[0] != n:
+        raise ValueError(f"k has {n} rows, v {v.shape[0]}")
+    _i32_dev(slots, "slots", dev, n)
+    _check(lib().milo_pages_store(p._as_parameter_, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(), n,
+                                  _stream_on(stream, dev)))
 
 
 def milo_pages_load(pages: MiloPages, slots, k_out=None, v_out=None, stream=None) -> None:
     """Rows of `slots` (int32 [n]) back to bf16 into k_out and / or v_out [n][H_kv][d]."""
     p = _pages_arg(pages)
-    _i32_dev(slots, "slots", (-1,))
+    dev, width = p.device.index, p.n_kv_heads * p.head_dim
+    _i32_dev(slots, "slots", dev, -1)
+    n = slots.shape[0]
     if k_out is None and v_out is None:
         raise ValueError("k_out and v_out are both None")
-    strides = [0, 0]
-    for i, (name, x) in enumerate((("k_out", k_out), ("v_out", v_out))):
-        if x is not None:
-            strides[i] = _row_stride(x, name, p.n_kv_heads, p.head_dim)
-            if x.shape[0] != slots.shape[0]:
-                raise ValueError(f"{name} has {x.shape[0]} rows, slots {slots.shape[0]}")
-            if x.shape[0] > 1 and strides[i] < p.n_kv_heads * p.head_dim:
-                raise ValueError(f"{name}'s rows overlap")
-    _check(lib().milo_pages_load(p._as_parameter_, slots.data_ptr(), int(slots.shape[0]), _addr(k_out), strides[0],
-                                 _addr(v_out), strides[1], _stream(stream)))
+    at = []
+    for name, x in (("k_out", k_out), ("v_out", v_out)):
+        if x is None:
+            at += [0, 0]
+            continue
+        stride = _row_stride(x, name, dev, p.n_kv_heads, p.head_dim)
+        if x.shape[0] != n:
+            raise ValueError(f"{name} has {x.shape[0]} rows, slots {n}")
+        if stride < width:
+            raise ValueError(f"{name}'s rows overlap")
+        at += [x.data_ptr(), stride]
+    _check(lib().milo_pages_load(p._as_parameter_, slots.data_ptr(), n, *at, _stream_on(stream, dev)))
 
 
 def milo_attend_pages(pages: MiloPages, page_table, lens, q, scale: float, out, *, q_starts=None, causal: bool = True,
@@ -606,36 +631,45 @@ def milo_attend_pages(pages: MiloPages, page_table, lens, q, scale: float, out, 
     milo_attend_pages_work(...) bytes, or None."""
     import torch
     p = _pages_arg(pages)
+    dev = p.device.index
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a bf16 GPU tensor [n_tok][H_q][d]")
-    n_tok, h_q = int(q.shape[0]), int(q.shape[1])
-    q_stride = _row_stride(q, "q", h_q, p.head_dim)
-    _dev_tensor(out, "out", ("torch.float32", "torch.bfloat16"), 3)
+    n_tok, h_q, d = q.shape
+    q_stride = _row_stride(q, "q", dev, h_q, p.head_dim)
+    if not isinstance(out, torch.Tensor) or out.dtype not in (torch.float32, torch.bfloat16) or out.get_device() != dev or \
+            not out.is_contiguous():
+        _dev_tensor(out, "out", ("torch.float32", "torch.bfloat16"))
     if out.shape != q.shape:
         raise ValueError(f"out shape {tuple(out.shape)} differs from q shape {tuple(q.shape)}")
-    _i32_dev(lens, "lens", (-1,))
-    n_req = int(lens.shape[0])
-    _i32_dev(page_table, "page_table", (n_req, -1))
+    _i32_dev(lens, "lens", dev, -1)
+    n_req = lens.shape[0]
+    _i32_dev(page_table, "page_table", dev, n_req, -1)
     if q_starts is not None:
-        _i32_dev(q_starts, "q_starts", (n_req + 1,))
-    table = None if block_table is None else np.asarray(block_table, dtype=np.int32).reshape(-1)
-    n_sel = 0 if table is None else int(table.size)
+        _i32_dev(q_starts, "q_starts", dev, n_req + 1)
+    table, n_sel = None, 0
+    if block_table is not None:
+        table = np.asarray(block_table, dtype=np.int32).reshape(-1)
+        n_sel = int(table.size)
     if cache is None:
         if n_sel:
             raise ValueError("block_table without a cache")
     elif cache not in _CACHES:
         raise ValueError("unknown cache handle (not created by milo_cache_create, or already freed)")
-    need = lib().milo_attend_pages_work(n_req, n_tok, h_q, p.n_kv_heads, p.head_dim, 1 if n_sel else 0)
+    L = lib()
+    need = L.milo_attend_pages_work(n_req, n_tok, h_q, p.n_kv_heads, d, 1 if n_sel else 0)
     if work is None:
-        with _on_stream(stream):
+        if stream is None:
             work = torch.empty(need, dtype=torch.uint8, device=q.device)
+        else:
+            with _on_stream(stream):
+                work = torch.empty(need, dtype=torch.uint8, device=q.device)
     elif _dev_tensor(work, "work", ("torch.uint8",)).numel() < need:
         raise ValueError(f"work holds {work.numel()} bytes, {need} are needed")
-    _check(lib().milo_attend_pages(
-        ctypes.c_void_p(cache), _i32(table) if n_sel else None, n_sel, p._as_parameter_, page_table.data_ptr(),
-        int(page_table.shape[1]), lens.data_ptr(), _addr(q_starts), n_req, q.data_ptr(), q_stride, n_tok, h_q,
-        1 if causal else 0, float(scale), out.data_ptr(), MILO_OUT_F32 if out.dtype == torch.float32 else MILO_OUT_BF16,
-        work.data_ptr(), _stream(stream)))
+    _check(L.milo_attend_pages(
+        cache, _i32(table) if n_sel else None, n_sel, p._as_parameter_, page_table.data_ptr(), page_table.shape[1],
+        lens.data_ptr(), _addr(q_starts), n_req, q.data_ptr(), q_stride, n_tok, h_q, 1 if causal else 0, scale,
+        out.data_ptr(), MILO_OUT_F32 if out.dtype is torch.float32 else MILO_OUT_BF16, work.data_ptr(),
+        _stream_on(stream, dev)))
 
 
 def milo_cache_free(cache: int | None) -> None:
