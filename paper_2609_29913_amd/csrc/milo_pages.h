@@ -78,9 +78,10 @@ inline int check_rows(const char* name, const void* p, int64_t stride, int64_t w
 // Request r's m queries are cut into column tiles of tt tokens; tile k sees vis(k) of
 // its n rows.  Positions number the work: request by request, KV head by KV head, tile
 // by tile, each tile kTileCost + vis(k) long (requests without queries take none).
-// Share w of W has the positions [w X / W, (w + 1) X / W) of X, in whatever tiles they
-// fall, so lengths may differ as they like; a tile's rows are cut at multiples of
-// kRowAlign.  All of it follows from the lengths, on the device.
+// Share w of W has the positions [w L, (w + 1) L) of X, L = ceil(X / W), in whatever tiles
+// they fall, so lengths may differ as they like (the last shares may be short or empty); a
+// tile's rows are cut at multiples of kRowAlign.  All of it follows from the lengths, on the
+// device.
 constexpr int kRowAlign = 64;
 constexpr int kTileCost = 128;  // what a tile costs besides its rows
 
@@ -112,9 +113,7 @@ __host__ __device__ inline int64_t request_cost(const Request& q, int tt, int ca
   return tiles_cost(q, (q.m + tt - 1) / tt, tt, causal);
 }
 
-__host__ __device__ inline int64_t share_begin(int w, int64_t X, int W) { return w * X / W; }
-// the share that holds position p: the largest w with floor(w X / W) <= p
-__host__ __device__ inline int share_holding(int64_t p, int64_t X, int W) { return (int)(((p + 1) * W + X - 1) / X) - 1; }
+__host__ __device__ inline int64_t share_length(int64_t X, int W) { return (X + W - 1) / W; }
 
 // the row at which boundary b cuts the tile at positions [p0, p1) that sees vis rows
 __host__ __device__ inline int row_at(int64_t b, int64_t p0, int64_t p1, int vis) {

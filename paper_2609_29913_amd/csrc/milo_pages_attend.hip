@@ -10,6 +10,10 @@
 namespace milo {
 namespace {
 
+constexpr int kPagesThreads = 256;   // four waves
+constexpr int kPagesWaves = kPagesThreads / 64;
+constexpr int kLeastRows = 256;      // positions of a share, at least
+
 struct PagesArgs {
   milo_pages p;
   const int32_t* table;
@@ -24,8 +28,8 @@ struct PagesArgs {
   float2* part_ml;         // their maxima (log2 units) and sums
   int4* meta;              // [grid] the tile that begins in a workgroup and ends in a later one
   float qscale;            // scale * log2(e)
-  int32_t min_rows;        // positions a workgroup gets at least,
-  int32_t min_wgs;         // unless fewer workgroups than this would work
+  int32_t least_tiles;     // what the host knows of the number of tiles
+  uint32_t G_inv;          // ceil(2^16 / G)
   int32_t whole_tiles;     // 1: a workgroup takes one whole tile, no shares
   int32_t n_req, n_tok, H_q, G, width, lg_page, causal, out_bf16;
 };
@@ -40,9 +44,6 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kPagesThreads = 256;   // four waves
-constexpr int kPagesWaves = kPagesThreads / 64;
 
 // eight codes as bf16, exactly
 template <int FMT>
@@ -111,6 +112,13 @@ __device__ inline Request request_of(const PagesArgs& a, int r) {
   return q;
 }
 
+// column c < 256 of a tile: its query and head (c < 256 and G <= 16: exact)
+__device__ inline int col_token(const PagesArgs& a, int c) { return (int)(c * a.G_inv >> 16); }
+__device__ inline int64_t col_offset(const PagesArgs& a, int c) {
+  const int tok = col_token(a, c);
+  return (int64_t)tok * a.H_q + c - tok * a.G;
+}
+
 // merges a column's result with the compressed context's and stores 4 dims of it
 __device__ inline void finish(const PagesArgs& a, int64_t col, int d, int D, float m, float l, float4 o) {
   if (a.ctx_ml) {
@@ -152,17 +160,24 @@ struct Window {
 constexpr float kMinValueScale = 1.262177448e-29f;  // 2^-96
 __device__ __forceinline__ bool no_values(float rv) { return __float_as_int(rv) < 0; }
 
-__device__ inline Window window_at(const PagesArgs& a, int req, int head, int base, int last_page) {
-  Window w;
+// Ids first, so that the codes' loads need not wait for the scales.
+__device__ inline void window_ids(const PagesArgs& a, int req, int base, int last_page, Window& w) {
   w.base = base;
-  const int pg = min(base + (int)(threadIdx.x & 63), last_page);
-  const int id = a.table[(int64_t)req * a.width + pg];
-  const bool in = (uint32_t)id < (uint32_t)a.p.n_pages;
-  w.id = in ? id : 0;
+  w.id = a.table[(int64_t)req * a.width + min(base + (int)(threadIdx.x & 63), last_page)];
+}
+
+__device__ inline void window_loads(const PagesArgs& a, int head, Window& w) {
+  const bool in = (uint32_t)w.id < (uint32_t)a.p.n_pages;
+  if (!in) w.id = 0;
   const int64_t at = (int64_t)w.id * a.p.n_kv_heads + head;
-  const float nan = __uint_as_float(0x7FC00000u);
-  const float vs = a.p.v_scale[at];
-  w.ks = in ? a.p.k_scale[at] * a.qscale : nan;
+  w.ks = a.p.k_scale[at];
+  w.lv = a.p.v_scale[at];
+  w.rv = in ? 1.f : __uint_as_float(0x7FC00000u);
+}
+
+__device__ inline void window_scales(const PagesArgs& a, Window& w) {
+  const float vs = w.lv, bad = w.rv;  // bad: 1, or NaN where the page is none
+  w.ks *= a.qscale * bad;
   w.lv = __builtin_amdgcn_logf(vs);
   w.rv = vs == vs ? exp2_hw(-w.lv) : 1.f;
   const bool none = vs < kMinValueScale;
@@ -176,7 +191,6 @@ __device__ inline Window window_at(const PagesArgs& a, int req, int head, int ba
       w.rv = -exp2_hw(-least);
     }
   }
-  return w;
 }
 
 // One step's codes (GS groups of 16 rows) and scales.
@@ -188,21 +202,14 @@ struct Step {
 };
 
 template <int D, int GS>
-__device__ __forceinline__ void load_step(const PagesArgs& a, int req, int head, Window& w, int row, int last_page,
-                                          Step<D, GS>& st) {
+__device__ __forceinline__ void load_codes(const PagesArgs& a, int head, const Window& w, int row, int last_page,
+                                           Step<D, GS>& st) {
   const int P = 1 << a.lg_page, lane = threadIdx.x & 63;
-  if ((row >> a.lg_page) - w.base >= 64) w = window_at(a, req, head, row >> a.lg_page, last_page);
   const int64_t head_bytes = (int64_t)P * D, page_bytes = head_bytes * a.p.n_kv_heads;
-  st.plain = true;
 #pragma unroll
   for (int g = 0; g < GS; ++g) {
-    const int r = row + 16 * g, pg = min(r >> a.lg_page, last_page), li = min(pg - w.base, 63);
-    const int id = lane_of(w.id, li);
-    st.ks[g] = lane_of(w.ks, li);
-    st.lv[g] = lane_of(w.lv, li);
-    st.rv[g] = lane_of(w.rv, li);
-    st.plain &= !no_values(st.rv[g]);
-    const int64_t at = id * page_bytes + head * head_bytes + (r & (P - 1)) * D;
+    const int r = row + 16 * g, li = min(min(r >> a.lg_page, last_page) - w.base, 63);
+    const int64_t at = lane_of(w.id, li) * page_bytes + head * head_bytes + (r & (P - 1)) * D;
     const uint8_t* kp = static_cast<const uint8_t*>(a.p.k_codes) + at;
     const uint8_t* vp = static_cast<const uint8_t*>(a.p.v_codes) + at;
 #pragma unroll
@@ -211,6 +218,31 @@ __device__ __forceinline__ void load_step(const PagesArgs& a, int req, int head,
       st.v[g][j] = *reinterpret_cast<const uint4*>(vp + 1024 * j + 16 * lane);
     }
   }
+}
+
+template <int D, int GS>
+__device__ __forceinline__ void take_scales(const PagesArgs& a, const Window& w, int row, int last_page, Step<D, GS>& st) {
+  st.plain = true;
+#pragma unroll
+  for (int g = 0; g < GS; ++g) {
+    const int li = min(min((row + 16 * g) >> a.lg_page, last_page) - w.base, 63);
+    st.ks[g] = lane_of(w.ks, li);
+    st.lv[g] = lane_of(w.lv, li);
+    st.rv[g] = lane_of(w.rv, li);
+    st.plain &= !no_values(st.rv[g]);
+  }
+}
+
+template <int D, int GS>
+__device__ __forceinline__ void load_step(const PagesArgs& a, int req, int head, Window& w, int row, int last_page,
+                                          Step<D, GS>& st) {
+  if ((row >> a.lg_page) - w.base >= 64) {
+    window_ids(a, req, row >> a.lg_page, last_page, w);
+    window_loads(a, head, w);
+    window_scales(a, w);
+  }
+  load_codes(a, head, w, row, last_page, st);
+  take_scales(a, w, row, last_page, st);
 }
 
 // A wave's running softmax over NT tiles of 16 columns: lane (n = l % 16, q = l / 16)
@@ -339,6 +371,7 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
   constexpr int COLS = SHARE ? 16 * NT : 16 * NT * kPagesWaves;
   constexpr int OS = D + 4;  // row stride of a column's partial in LDS
   __shared__ int64_t pre[kPagesThreads + 1];
+  __shared__ Request reqs[kPagesThreads];  // all of them where there are no more than threads
   // two sets in turn: a wave writes a tile's while others still read the last one's
   __shared__ float joined[2][2][kPagesWaves][16 * NT];
   __shared__ __align__(16) float part[SHARE ? kPagesWaves * 16 * NT * OS : 4];
@@ -351,6 +384,7 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
     int64_t own = 0;
     for (int r = tid * chunk; r < min((tid + 1) * chunk, a.n_req); ++r) {
       const Request q = request_of(a, r);
+      reqs[tid] = q;
       own += a.whole_tiles ? (q.m + tt - 1) / tt : request_cost(q, tt, a.causal);
     }
     int64_t inc = own;
@@ -371,21 +405,27 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
   const int64_t X = uniform(H * pre[kPagesThreads]);
   // (a share is at least kTileCost long, so none is empty)
   if (a.whole_tiles && blockIdx.x >= X) return;
-  int W = (int)min(min((int64_t)gridDim.x, X / kTileCost), max(X / a.min_rows, (int64_t)a.min_wgs));
+  // As many shares as keep kLeastRows each, up to the grid; one for a tile where that is
+  // about as many, so that tiles of like length are not cut.
+  int64_t want = X / kLeastRows;
+  if (want < 2 * a.least_tiles) want = a.least_tiles;
+  int W = (int)min(min((int64_t)gridDim.x, X / kTileCost), want);
   if (W >= kXcds) W -= W % kXcds;
+  const int64_t L = uniform(share_length(X, max(W, 1)));
   int4* meta = a.meta + blockIdx.x;
-  if (!a.whole_tiles) {
-    if (tid == 0) *meta = make_int4(-1, 0, 0, 0);
-    if ((int)blockIdx.x >= W || X == 0) return;
-  }
   // consecutive shares on one XCD, whose L2 then holds the rows that tiles share
   const int w = W >= kXcds ? (int)(blockIdx.x % kXcds) * (W / kXcds) + blockIdx.x / kXcds : blockIdx.x;
-  int64_t b0 = uniform(share_begin(w, X, W)), b1 = uniform(share_begin(w + 1, X, W));
-  if (a.whole_tiles) b0 = blockIdx.x;
+  int64_t b0 = uniform(w * L), b1 = min(b0 + L, X);
+  if (!a.whole_tiles) {
+    if (tid == 0) *meta = make_int4(-1, 0, 0, 0);
+    if ((int)blockIdx.x >= W || b0 >= X) return;
+  } else {
+    b0 = blockIdx.x;
+  }
 
   // the tile that b0 falls in
   Place at;
-  const auto get = [&](int r) { return request_of(a, r); };
+  const auto get = [&](int r) { return chunk == 1 ? reqs[r] : request_of(a, r); };
   {
     int lo = 0, hi = kPagesThreads;
     while (hi - lo > 1) {
@@ -398,7 +438,7 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
     } else {  // a request's last tiles, which see most, first; its heads side by side
       int x = (int)(b0 - H * pre[lo]), n_tiles;
       for (at.r = lo * chunk;; ++at.r) {
-        at.rq = request_of(a, at.r);
+        at.rq = get(at.r);
         n_tiles = (at.rq.m + tt - 1) / tt;
         if (x < H * n_tiles) break;
         x -= H * n_tiles;
@@ -433,19 +473,23 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
       wa = ra + steps * wave / kPagesWaves * ROWS;
       wb = min(rb, ra + steps * (wave + 1) / kPagesWaves * ROWS);
     }
+    const bool works = wa < wb && col0 < ncol;
+    const int last_page = (n - 1) >> a.lg_page;
+    Window win;
+    if (works) window_ids(a, req, wa >> a.lg_page, last_page, win);
     Running<D, NT> run;
     int vis[NT], vis_lo = n;
     bf16x8 qf[NT][D / 32];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int c = col0 + 16 * t + (lane & 15), tok = c / a.G;
+      const int c = col0 + 16 * t + (lane & 15), tok = col_token(a, c);
       vis[t] = 0;
 #pragma unroll
       for (int k = 0; k < D / 32; ++k) qf[t][k] = bf16x8{};
       if (c < ncol) {
         const Request me{start, m, n};
         vis[t] = seen_upto(me, j0 + tok + 1, a.causal);
-        const uint16_t* src = a.q + (int64_t)(start + j0 + tok) * a.q_stride + (int64_t)(g * a.G + c % a.G) * D;
+        const uint16_t* src = a.q + (int64_t)(start + j0 + tok) * a.q_stride + (int64_t)(g * a.G + c - tok * a.G) * D;
 #pragma unroll
         for (int k = 0; k < D / 32; ++k)
           qf[t][k] = *reinterpret_cast<const bf16x8*>(src + 64 * (k / 2) + 16 * (lane >> 4) + 8 * (k % 2));
@@ -458,16 +502,17 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
     // steps below vis_lo need no mask: the fewest rows a column of this wave sees
     if (col0 < ncol) {
       const Request me{start, m, n};
-      vis_lo = seen_upto(me, j0 + col0 / a.G + 1, a.causal);
+      vis_lo = seen_upto(me, j0 + col_token(a, col0) + 1, a.causal);
     }
     vis_lo = uniform(vis_lo);
     wa = uniform(wa);
     wb = uniform(wb);
-    if (wa < wb && col0 < ncol) {
-      const int last_page = (n - 1) >> a.lg_page;
-      Window win = window_at(a, req, g, wa >> a.lg_page, last_page);
+    if (works) {
       Step<D, GS> s0, s1;
-      load_step(a, req, g, win, wa, last_page, s0);
+      window_loads(a, g, win);
+      load_codes(a, g, win, wa, last_page, s0);
+      window_scales(a, win);
+      take_scales(a, win, wa, last_page, s0);
       int row = wa;
       for (; row + 2 * ROWS <= min(vis_lo, wb) && s0.plain; row += 2 * ROWS) {
         load_step(a, req, g, win, row + ROWS, last_page, s1);
@@ -534,7 +579,7 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
           o.w += y.w;
         }
         if (whole) {
-          finish(a, q0 + (int64_t)(c / a.G) * a.H_q + c % a.G, d, D, mx, l, o);
+          finish(a, q0 + col_offset(a, c), d, D, mx, l, o);
         } else {
           *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * COLS + c) * D + d) = o;
           if (d == 0) a.part_ml[(int64_t)slot * COLS + c] = make_float2(mx, l);
@@ -549,7 +594,7 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
           for (int k = 0; k < D / 16; ++k) {
             const int d = 16 * k + 4 * (lane >> 4);
             const float4 o = make_float4(run.o[t][k][0], run.o[t][k][1], run.o[t][k][2], run.o[t][k][3]);
-            if (whole) finish(a, q0 + (int64_t)(c / a.G) * a.H_q + c % a.G, d, D, run.m[t], run.l[t], o);
+            if (whole) finish(a, q0 + col_offset(a, c), d, D, run.m[t], run.l[t], o);
             else *reinterpret_cast<float4*>(a.part_o + ((int64_t)slot * COLS + c) * D + d) = o;
           }
           if (!whole && lane < 16) a.part_ml[(int64_t)slot * COLS + c] = make_float2(run.m[t], run.l[t]);
@@ -558,7 +603,7 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
     }
     // a tile that begins here and goes on in the next workgroups: joined afterwards
     if (tid == 0 && b0 <= p0 && b1 < p1) {
-      const int we = share_holding(p1 - 1, X, W);
+      const int we = (int)((p1 - 1) / L);
       *meta = make_int4((int)q0, ncol, slot, we);
     }
     first = false;
@@ -567,21 +612,11 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
   }
 }
 
-// Joins the parts of the tile that begins in share w and ends in share we: its own
-// slot and the first slot of the shares after it.  A workgroup takes a column at a
-// time; its lanes of D / 4 threads take every PL-th part in turn, four at once, and
-// are joined in order.
-template <int D, int COLS>
-__global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) {
-  constexpr int TPC = D / 4, PL = kPagesThreads / TPC, U = 4;
-  __shared__ float2 lane_ml[PL];
-  __shared__ float4 lane_o[PL][TPC];
-  const int4 mt = a.meta[blockIdx.x];
-  if (mt.x < 0) return;
-  const int s0 = mt.z, we = mt.w, w = s0 >> 1, dq = threadIdx.x % TPC, pl = threadIdx.x / TPC;
-  float m, l;
-  float4 o;
-  const auto add = [&](float2 ml, const float4& y) {
+// A column's sums as parts are added to them, each relative to 2^m.
+struct Joined {
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ void add(float2 ml, const float4& y) {
     if (ml.x == -INFINITY && ml.y == 0.f) return;  // a part without rows
     const float mx = fmaxf(m, ml.x);
     const float f = m == -INFINITY ? 1.f : exp2_hw(m - mx), fy = ml.x == -INFINITY ? 1.f : exp2_hw(ml.x - mx);
@@ -591,32 +626,71 @@ __global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) 
     o.z = o.z * f + y.z * fy;
     o.w = o.w * f + y.w * fy;
     m = mx;
-  };
-  for (int c = blockIdx.y; c < mt.y; c += gridDim.y) {
-    m = -INFINITY;
-    l = 0.f;
-    o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = w + pl; k0 <= we; k0 += PL * U) {
-      float2 ml[U];
-      float4 y[U];
+  }
+};
+
+// Joins the parts of the tile that begins in share w and ends in share we: its own
+// slot and the first slot of the shares after it.  Of few parts, a workgroup's PL lanes
+// of D / 4 threads take a column each; of many, they share CB columns at a time, each
+// every PL-th part in turn, U at once, and are joined in order.
+template <int D, int COLS>
+__global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) {
+  constexpr int TPC = D / 4, PL = kPagesThreads / TPC, U = 4, CB = 4;
+  static_assert(CB <= PL, "a lane finishes a column");
+  __shared__ float2 lane_ml[PL][CB];
+  __shared__ float4 lane_o[PL][CB][TPC];
+  const int4 mt = a.meta[blockIdx.x];
+  if (mt.x < 0) return;
+  const int s0 = mt.z, we = mt.w, w = s0 >> 1, dq = threadIdx.x % TPC, pl = threadIdx.x / TPC;
+  const auto part_at = [&](int k, int c) { return (int64_t)(k == w ? s0 : 2 * k) * COLS + c; };
+  if (we - w < 2 * U) {
+    for (int c = blockIdx.y * PL + pl; c < mt.y; c += gridDim.y * PL) {
+      float2 ml[2 * U];
+      float4 y[2 * U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = min(k0 + u * PL, we);
-        const int64_t at = (int64_t)(k == w ? s0 : 2 * k) * COLS + c;
+      for (int u = 0; u < 2 * U; ++u) {
+        const int64_t at = part_at(min(w + u, we), c);
         ml[u] = a.part_ml[at];
         y[u] = *reinterpret_cast<const float4*>(a.part_o + at * D + 4 * dq);
       }
+      Joined s;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (k0 + u * PL <= we) add(ml[u], y[u]);
+      for (int u = 0; u < 2 * U; ++u)
+        if (w + u <= we) s.add(ml[u], y[u]);
+      finish(a, mt.x + col_offset(a, c), 4 * dq, D, s.m, s.l, s.o);
     }
-    if (dq == 0) lane_ml[pl] = make_float2(m, l);
-    lane_o[pl][dq] = o;
-    __syncthreads();
-    if (pl == 0) {
+    return;
+  }
+  for (int c0 = blockIdx.y * CB; c0 < mt.y; c0 += gridDim.y * CB) {
+    Joined s[CB];
+    for (int k0 = w + pl; k0 <= we; k0 += PL * U) {
+      float2 ml[CB][U];
+      float4 y[CB][U];
 #pragma unroll
-      for (int k = 1; k < PL; ++k) add(lane_ml[k], lane_o[k][dq]);
-      finish(a, mt.x + (int64_t)(c / a.G) * a.H_q + c % a.G, 4 * dq, D, m, l, o);
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int64_t at = part_at(min(k0 + u * PL, we), min(c0 + c, mt.y - 1));
+          ml[c][u] = a.part_ml[at];
+          y[c][u] = *reinterpret_cast<const float4*>(a.part_o + at * D + 4 * dq);
+        }
+#pragma unroll
+      for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (k0 + u * PL <= we) s[c].add(ml[c][u], y[c][u]);
+    }
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+      if (dq == 0) lane_ml[pl][c] = make_float2(s[c].m, s[c].l);
+      lane_o[pl][c][dq] = s[c].o;
+    }
+    __syncthreads();
+    if (pl < CB && c0 + pl < mt.y) {
+      Joined all;
+#pragma unroll
+      for (int k = 0; k < PL; ++k) all.add(lane_ml[k][pl], lane_o[k][pl][dq]);
+      finish(a, mt.x + col_offset(a, c0 + pl), 4 * dq, D, all.m, all.l, all.o);
     }
     __syncthreads();
   }
@@ -653,9 +727,11 @@ void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
     else launch_pages<D, MILO_KV_INT8, 2>(a, t, grid, s);
   }
   if (a.whole_tiles) return;
-  if (t == kFew) hipLaunchKernelGGL((pages_join_kernel<D, 16>), dim3(kGrid, 8), dim3(kPagesThreads), 0, s, a);
-  else if (t == kSome) hipLaunchKernelGGL((pages_join_kernel<D, 64>), dim3(kGrid, 16), dim3(kPagesThreads), 0, s, a);
-  else hipLaunchKernelGGL((pages_join_kernel<D, 128>), dim3(kGrid, 16), dim3(kPagesThreads), 0, s, a);
+  // where tiles are few, each is in many parts, and more workgroups share a join
+  const int y = a.least_tiles >= kGrid / 8 ? (t == kFew ? 1 : 4) : 8;
+  if (t == kFew) hipLaunchKernelGGL((pages_join_kernel<D, 16>), dim3(kGrid, y), dim3(kPagesThreads), 0, s, a);
+  else if (t == kSome) hipLaunchKernelGGL((pages_join_kernel<D, 64>), dim3(kGrid, y), dim3(kPagesThreads), 0, s, a);
+  else hipLaunchKernelGGL((pages_join_kernel<D, 128>), dim3(kGrid, y), dim3(kPagesThreads), 0, s, a);
 }
 
 }  // namespace
@@ -757,8 +833,8 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   const int tt = tile_columns(tiling) / G;
   const int64_t least = (int64_t)H * std::max((n_tok + tt - 1) / tt, std::min(n_req, n_tok));
   const int64_t most = (int64_t)H * (n_tok / tt + std::min(n_req, n_tok));
-  a.min_rows = 256;
-  a.min_wgs = (int)std::min<int64_t>(kGrid, least);
+  a.least_tiles = (int)std::min<int64_t>(kGrid, least);
+  a.G_inv = (65536 + G - 1) / G;
   a.whole_tiles = tiling != kFew && least >= kGrid / 2;
   const int grid = a.whole_tiles ? (int)most : kGrid;
   if (d == 64) launch_pages<64>(a, tiling, grid, s);

@@ -62,9 +62,11 @@ int main() {
     // the tiles in order, each with the row up to which it is done
     int r = 0, head = 0, tile = 0, done = 0, parts = 0, last_end = -1;
     while (req[r].m == 0) ++r;
+    const int64_t L = share_length(X, W);
+    CHECK((X + L - 1) / L <= W);
     for (int w = 0; w < W; ++w) {
-      const int64_t b0 = share_begin(w, X, W), b1 = share_begin(w + 1, X, W);
-      CHECK(b0 < b1);
+      const int64_t b0 = w * L, b1 = std::min(b0 + L, X);
+      if (b0 >= X) continue;
       int lo = 0;
       while (pre[lo + 1] <= b0) ++lo;
       lo = lo > 2 ? lo - pick(0, 2) : lo;  // any request before will do
@@ -79,10 +81,10 @@ int main() {
         CHECK(p0 <= pos && pos < p1 && (first || p0 == pos));
         const int ra = row_at(b0, p0, p1, vis), rb = row_at(b1, p0, p1, vis);
         CHECK(ra == done && ra <= rb && rb <= vis && (ra % kRowAlign == 0 || ra == vis));
-        CHECK(share_holding(pos, X, W) == w && share_holding(std::min(p1, b1) - 1, X, W) == w);
+        CHECK(pos / L == w && (std::min(p1, b1) - 1) / L == w);
         const bool whole = b0 <= p0 && b1 >= p1;
         CHECK(!whole || (ra == 0 && rb == vis && parts == 0));
-        if (!whole && b0 <= p0) last_end = share_holding(p1 - 1, X, W);
+        if (!whole && b0 <= p0) last_end = (int)((p1 - 1) / L);
         if (!whole) CHECK(parts == 0 ? b0 <= p0 && b1 < p1 : first);
         done = rb;
         ++parts;
