@@ -367,14 +367,16 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
 // (64 NT columns, every wave reads all rows).
 template <int D, int FMT, int PARTS, int NT, bool SHARE>
 __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
-  constexpr int GS = SHARE ? 4 : 2, ROWS = 16 * GS;
+  constexpr int GS = NT == 1 ? 4 : 2, ROWS = 16 * GS;
   constexpr int COLS = SHARE ? 16 * NT : 16 * NT * kPagesWaves;
   constexpr int OS = D + 4;  // row stride of a column's partial in LDS
   __shared__ int64_t pre[kPagesThreads + 1];
   __shared__ Request reqs[kPagesThreads];  // all of them where there are no more than threads
   // two sets in turn: a wave writes a tile's while others still read the last one's
   __shared__ float joined[2][2][kPagesWaves][16 * NT];
-  __shared__ __align__(16) float part[SHARE ? kPagesWaves * 16 * NT * OS : 4];
+  // waves' sums on their way together: all four waves', or, of 32 columns, two at a time
+  constexpr int PW = NT == 1 ? kPagesWaves : kPagesWaves / 2;
+  __shared__ __align__(16) float part[SHARE ? PW * 16 * NT * OS : 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int tt = COLS / a.G, H = a.p.n_kv_heads;
 
@@ -556,10 +558,27 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
         for (int k = 1; k < kPagesWaves; ++k) mx = fmaxf(mx, wave_m[k][c]);
         const float f = run.m[t] == -INFINITY ? 1.f : exp2_hw(run.m[t] - mx);
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const f32x4 o = run.o[t][k] * f;
-          *reinterpret_cast<f32x4*>(&part[(wave * 16 * NT + c) * OS + 16 * k + 4 * (lane >> 4)]) = o;
+        for (int k = 0; k < D / 16; ++k) run.o[t][k] *= f;
+      }
+      float* mine = &part[((wave & (PW - 1)) * 16 * NT + (lane & 15)) * OS + 4 * (lane >> 4)];
+      const auto put = [&] {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) *reinterpret_cast<f32x4*>(mine + 16 * t * OS + 16 * k) = run.o[t][k];
+      };
+      if constexpr (PW < kPagesWaves) {
+        if (wave >= PW) put();
+        __syncthreads();
+        if (wave < PW) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) run.o[t][k] += *reinterpret_cast<const f32x4*>(mine + 16 * t * OS + 16 * k);
+          put();  // where it has read
         }
+      } else {
+        put();
       }
       __syncthreads();
       for (int x = tid; x < ncol * (D / 4); x += kPagesThreads) {
@@ -572,6 +591,9 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
         for (int k = 0; k < kPagesWaves; ++k) {
           const float wm = wave_m[k][c];
           l += wave_l[k][c] * (wm == -INFINITY ? 1.f : exp2_hw(wm - mx));
+        }
+#pragma unroll
+        for (int k = 0; k < PW; ++k) {
           const float4 y = *reinterpret_cast<const float4*>(&part[(k * 16 * NT + c) * OS + d]);
           o.x += y.x;
           o.y += y.y;
@@ -700,19 +722,19 @@ int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
 
 constexpr int kGrid = 512;  // workgroups that share the work: two on every CU
 
-// How a call's columns are tiled: 16 to a workgroup whose waves split the rows where
-// requests bring few queries each, else 64 or 128 whose waves split the columns.
+// How a call's columns are tiled: 16 or 32 to a workgroup whose waves split the rows where
+// requests bring few queries each, else 128 whose waves split the columns.
 enum Tiling { kFew, kSome, kMany };
 Tiling tiling_of(int32_t n_req, int32_t n_tok, int G) {
   const int64_t cols = (int64_t)n_tok * G;
-  return cols <= 24 * (int64_t)n_req ? kFew : cols <= 64 * (int64_t)n_req ? kSome : kMany;
+  return cols <= 16 * (int64_t)n_req ? kFew : cols <= 112 * (int64_t)n_req ? kSome : kMany;
 }
-int tile_columns(Tiling t) { return t == kFew ? 16 : t == kSome ? 64 : 128; }
+int tile_columns(Tiling t) { return t == kFew ? 16 : t == kSome ? 32 : 128; }
 
 template <int D, int FMT, int PARTS>
 void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
   if (t == kFew) hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 1, true>), dim3(grid), dim3(kPagesThreads), 0, s, a);
-  else if (t == kSome) hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 1, false>), dim3(grid), dim3(kPagesThreads), 0, s, a);
+  else if (t == kSome) hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 2, true>), dim3(grid), dim3(kPagesThreads), 0, s, a);
   else hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 2, false>), dim3(grid), dim3(kPagesThreads), 0, s, a);
 }
 
@@ -728,9 +750,9 @@ void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
   }
   if (a.whole_tiles) return;
   // where tiles are few, each is in many parts, and more workgroups share a join
-  const int y = a.least_tiles >= kGrid / 8 ? (t == kFew ? 1 : 4) : 8;
+  const int y = a.least_tiles >= kGrid / 8 ? (t == kMany ? 4 : 1) : 8;
   if (t == kFew) hipLaunchKernelGGL((pages_join_kernel<D, 16>), dim3(kGrid, y), dim3(kPagesThreads), 0, s, a);
-  else if (t == kSome) hipLaunchKernelGGL((pages_join_kernel<D, 64>), dim3(kGrid, y), dim3(kPagesThreads), 0, s, a);
+  else if (t == kSome) hipLaunchKernelGGL((pages_join_kernel<D, 32>), dim3(kGrid, y), dim3(kPagesThreads), 0, s, a);
   else hipLaunchKernelGGL((pages_join_kernel<D, 128>), dim3(kGrid, y), dim3(kPagesThreads), 0, s, a);
 }
 
