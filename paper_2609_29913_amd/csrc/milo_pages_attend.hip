@@ -267,19 +267,25 @@ template <bool MASKED, int D, int FMT, int PARTS, int NT, int GS>
 __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&qf)[NT][D / 32], int row,
                                          int n, const int (&vis)[NT], Running<D, NT>& run) {
   const int lane = threadIdx.x & 63, q4 = (lane >> 4) * 4;
+  // two groups at a time: as many independent sums as hide a product's latency
   f32x4 s[GS][NT];
 #pragma unroll
-  for (int g = 0; g < GS; ++g) {
+  for (int g0 = 0; g0 < GS; g0 += 2) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) s[g][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int g = g0; g < g0 + 2; ++g)
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) {
-      const bf16x8 a0 = codes_bf16<FMT>(st.k[g][j].x, st.k[g][j].y), a1 = codes_bf16<FMT>(st.k[g][j].z, st.k[g][j].w);
+      for (int t = 0; t < NT; ++t) s[g][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int t = 0; t < NT; ++t) s[g][t] = mfma16(a0, qf[t][2 * j], s[g][t]);
+    for (int j = 0; j < D / 64; ++j)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) s[g][t] = mfma16(a1, qf[t][2 * j + 1], s[g][t]);
-    }
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int g = g0; g < g0 + 2; ++g) {
+          const uint4& raw = st.k[g][j];
+          const bf16x8 kf = half == 0 ? codes_bf16<FMT>(raw.x, raw.y) : codes_bf16<FMT>(raw.z, raw.w);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) s[g][t] = mfma16(kf, qf[t][2 * j + half], s[g][t]);
+        }
     __builtin_amdgcn_sched_barrier(0);
   }
   // the conversions of the phases stay in them: moved up, they cost registers (spills)
@@ -655,9 +661,9 @@ struct Joined {
 // slot and the first slot of the shares after it.  Of few parts, a workgroup's PL lanes
 // of D / 4 threads take a column each; of many, they share CB columns at a time, each
 // every PL-th part in turn, U at once, and are joined in order.
-template <int D, int COLS>
+template <int D, int COLS, int CB>
 __global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) {
-  constexpr int TPC = D / 4, PL = kPagesThreads / TPC, U = 4, CB = 4;
+  constexpr int TPC = D / 4, PL = kPagesThreads / TPC, U = 4;
   static_assert(CB <= PL, "a lane finishes a column");
   __shared__ float2 lane_ml[PL][CB];
   __shared__ float4 lane_o[PL][CB][TPC];
@@ -738,6 +744,16 @@ void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
   else hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 2, false>), dim3(grid), dim3(kPagesThreads), 0, s, a);
 }
 
+template <int D, int COLS>
+void launch_join(const PagesArgs& a, hipStream_t s) {
+  // Where tiles are few, each is in many parts: a workgroup for each column.  Most
+  // workgroups of the grid find no tile and leave.
+  if (a.least_tiles < kGrid / 8)
+    hipLaunchKernelGGL((pages_join_kernel<D, COLS, 1>), dim3(kGrid, 16), dim3(kPagesThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((pages_join_kernel<D, COLS, 4>), dim3(kGrid, COLS / 32 + 1), dim3(kPagesThreads), 0, s, a);
+}
+
 template <int D>
 void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
   const bool e4m3 = a.p.format == MILO_KV_E4M3;
@@ -749,11 +765,9 @@ void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
     else launch_pages<D, MILO_KV_INT8, 2>(a, t, grid, s);
   }
   if (a.whole_tiles) return;
-  // where tiles are few, each is in many parts, and more workgroups share a join
-  const int y = a.least_tiles >= kGrid / 8 ? (t == kMany ? 4 : 1) : 8;
-  if (t == kFew) hipLaunchKernelGGL((pages_join_kernel<D, 16>), dim3(kGrid, y), dim3(kPagesThreads), 0, s, a);
-  else if (t == kSome) hipLaunchKernelGGL((pages_join_kernel<D, 32>), dim3(kGrid, y), dim3(kPagesThreads), 0, s, a);
-  else hipLaunchKernelGGL((pages_join_kernel<D, 128>), dim3(kGrid, y), dim3(kPagesThreads), 0, s, a);
+  if (t == kFew) launch_join<D, 16>(a, s);
+  else if (t == kSome) launch_join<D, 32>(a, s);
+  else launch_join<D, 128>(a, s);
 }
 
 }  // namespace
