@@ -74,20 +74,28 @@ inline int check_rows(const char* name, const void* p, int64_t stride, int64_t w
   return MILO_OK;
 }
 
-// ---- the work of an attention call, in rows ---------------------------------------
+// ---- the work of an attention call -------------------------------------------------
 // Request r's m queries are cut into column tiles of tt tokens; tile k sees vis(k) of
-// its n rows.  Positions number the work: request by request, KV head by KV head, tile
-// by tile, each tile kTileCost + vis(k) long (requests without queries take none).
+// its n rows.  Positions number the work, kRowAlign rows each: request by request, KV
+// head by KV head, tile by tile, the first k tiles of a head kTileCost k + (vis(0) + ..
+// + vis(k - 1)) / kRowAlign long, rounded down (requests without queries take none).
 // Share w of W has the positions [w L, (w + 1) L) of X, L = ceil(X / W), in whatever tiles
 // they fall, so lengths may differ as they like (the last shares may be short or empty); a
 // tile's rows are cut at multiples of kRowAlign.  All of it follows from the lengths, on the
-// device.
+// device; the host sees to it that X fits 31 bits.
 constexpr int kRowAlign = 64;
-constexpr int kTileCost = 128;  // what a tile costs besides its rows
+constexpr int kTileCost = 2;  // what a tile costs besides its rows
 
 struct Request {
   int start, m, n;  // first query, queries, rows held
 };
+
+// ceil(x / tt) for x <= 2^24 and tt <= 128 by the reciprocal ceil(2^32 / tt) (0 for tt = 1)
+__host__ __device__ inline int tiles_of(int m, int tt, uint32_t tt_inv) {
+  const uint32_t x = (uint32_t)(m + tt - 1);
+  return tt == 1 ? (int)x : (int)(((uint64_t)x * tt_inv) >> 32);
+}
+inline uint32_t reciprocal(int tt) { return (uint32_t)((((uint64_t)1 << 32) + tt - 1) / tt); }
 
 // rows that query number j - 1 of the request sees (at most its last one's)
 __host__ __device__ inline int seen_upto(const Request& q, int j, int causal) {
@@ -96,72 +104,82 @@ __host__ __device__ inline int seen_upto(const Request& q, int j, int causal) {
   return v > 0 ? v : 0;
 }
 
-// positions of the first k of a request's tiles
-__host__ __device__ inline int64_t tiles_cost(const Request& q, int k, int tt, int causal) {
+// positions of the first k of a request's `all` tiles
+__host__ __device__ inline int tiles_cost(const Request& q, int k, int all, int tt, int causal) {
   if (k <= 0) return 0;
-  if (!causal) return (int64_t)k * (kTileCost + q.n);
-  // tile i sees max(0, base + (i + 1) tt) rows, the request's last tile n
-  const int all = (q.m + tt - 1) / tt, whole = k < all ? k : all - 1;
-  const int64_t base = (int64_t)q.n - q.m;
-  int64_t skip = base < 0 ? -base / tt : 0;  // tiles that see nothing
-  if (skip > whole) skip = whole;
-  int64_t sum = (whole - skip) * base + (int64_t)tt * (whole * ((int64_t)whole + 1) / 2 - skip * (skip + 1) / 2);
-  if (k >= all) sum += q.n;
-  return sum + (int64_t)k * kTileCost;
+  int64_t sum;
+  if (!causal) {
+    sum = (int64_t)k * q.n;
+  } else {
+    // tile i sees max(0, base + (i + 1) tt) rows, the request's last tile n
+    const int whole = k < all ? k : all - 1, base = q.n - q.m;
+    int skip = base < 0 ? -base / tt : 0;  // tiles that see nothing
+    if (skip > whole) skip = whole;
+    sum = (int64_t)(whole - skip) * base + (int64_t)tt * (((int64_t)whole * (whole + 1) - (int64_t)skip * (skip + 1)) / 2);
+    if (k >= all) sum += q.n;
+  }
+  return (int)(sum / kRowAlign) + k * kTileCost;
 }
-__host__ __device__ inline int64_t request_cost(const Request& q, int tt, int causal) {
-  return tiles_cost(q, (q.m + tt - 1) / tt, tt, causal);
-}
-
-__host__ __device__ inline int64_t share_length(int64_t X, int W) { return (X + W - 1) / W; }
 
 // the row at which boundary b cuts the tile at positions [p0, p1) that sees vis rows
-__host__ __device__ inline int row_at(int64_t b, int64_t p0, int64_t p1, int vis) {
-  if (b <= p0 + kTileCost) return 0;
+__host__ __device__ inline int row_at(int b, int p0, int p1, int vis) {
   if (b >= p1) return vis;
-  return (int)(b - p0 - kTileCost) & ~(kRowAlign - 1);
+  if (b <= p0 + kTileCost) return 0;
+  return (b - p0 - kTileCost) * kRowAlign;
 }
 
 struct Place {
-  int r, head, tile;
-  int64_t p;   // first position of the tile
+  int r, head, tile, all;  // all: tiles of the request
+  int p0, p1;              // positions of the tile
+  int head0, cost;         // first position of the head's tiles, and how many
   Request rq;
 };
 
+// sets the positions of the tile that `at` names
+__host__ __device__ inline void set_tile(Place& at, int tt, int causal) {
+  at.p0 = at.head0 + tiles_cost(at.rq, at.tile, at.all, tt, causal);
+  at.p1 = at.tile + 1 < at.all ? at.head0 + tiles_cost(at.rq, at.tile + 1, at.all, tt, causal) : at.head0 + at.cost;
+}
+
 // the tile that holds position b, where request r0's work begins at p <= b
 template <typename Get>
-__host__ __device__ inline Place place_of(const Get& get, int r0, int64_t p, int64_t b, int H, int tt, int causal) {
+__host__ __device__ inline Place place_of(const Get& get, int r0, int p, int b, int H, int tt, uint32_t tt_inv, int causal) {
   Place at;
-  int64_t cost;
   for (at.r = r0;; ++at.r) {
     at.rq = get(at.r);
-    cost = request_cost(at.rq, tt, causal);
-    if (b < p + H * cost) break;
-    p += H * cost;
+    at.all = tiles_of(at.rq.m, tt, tt_inv);
+    at.cost = tiles_cost(at.rq, at.all, at.all, tt, causal);
+    if (b - p < H * at.cost) break;
+    p += H * at.cost;
   }
-  at.head = (int)((b - p) / cost);
-  p += at.head * cost;
-  int t0 = 0, t1 = (at.rq.m + tt - 1) / tt;
+  at.head = (int)((uint32_t)(b - p) / (uint32_t)at.cost);
+  at.head0 = p + at.head * at.cost;
+  int t0 = 0, t1 = at.all;
   while (t1 - t0 > 1) {
     const int mid = (t0 + t1) >> 1;
-    if (p + tiles_cost(at.rq, mid, tt, causal) <= b) t0 = mid;
+    if (at.head0 + tiles_cost(at.rq, mid, at.all, tt, causal) <= b) t0 = mid;
     else t1 = mid;
   }
   at.tile = t0;
-  at.p = p + tiles_cost(at.rq, t0, tt, causal);
+  set_tile(at, tt, causal);
   return at;
 }
 
-// the tile after, which begins at p (there is one)
+// the tile after (there is one)
 template <typename Get>
-__host__ __device__ inline void next_tile(const Get& get, Place& at, int64_t p, int H, int tt) {
-  at.p = p;
-  if (++at.tile < (at.rq.m + tt - 1) / tt) return;
-  at.tile = 0;
-  if (++at.head < H) return;
-  at.head = 0;
-  do at.rq = get(++at.r);
-  while (at.rq.m == 0);
+__host__ __device__ inline void next_tile(const Get& get, Place& at, int H, int tt, uint32_t tt_inv, int causal) {
+  if (++at.tile >= at.all) {
+    at.tile = 0;
+    at.head0 += at.cost;
+    if (++at.head >= H) {
+      at.head = 0;
+      do at.rq = get(++at.r);
+      while (at.rq.m == 0);
+      at.all = tiles_of(at.rq.m, tt, tt_inv);
+      at.cost = tiles_cost(at.rq, at.all, at.all, tt, causal);
+    }
+  }
+  set_tile(at, tt, causal);
 }
 
 #ifdef __HIPCC__

@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kPagesThreads = 256;   // four waves
 constexpr int kPagesWaves = kPagesThreads / 64;
-constexpr int kLeastRows = 256;      // positions of a share, at least
+constexpr int kLeastShare = 4;       // positions (64 rows each) of a share, as a rule
 
 struct PagesArgs {
   milo_pages p;
@@ -29,7 +29,7 @@ struct PagesArgs {
   int4* meta;              // [grid] the tile that begins in a workgroup and ends in a later one
   float qscale;            // scale * log2(e)
   int32_t least_tiles;     // what the host knows of the number of tiles
-  uint32_t G_inv;          // ceil(2^16 / G)
+  uint32_t G_inv, tt_inv;  // ceil(2^16 / G), ceil(2^32 / tt) (tiles_of)
   int32_t whole_tiles;     // 1: a workgroup takes one whole tile, no shares
   int32_t n_req, n_tok, H_q, G, width, lg_page, causal, out_bf16;
 };
@@ -96,8 +96,15 @@ __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
 }
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+// sums of x over the lanes up to this one
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // from 1, 2, 4, 8 lanes before, in rows of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // rows 0 and 2 to rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // row 1 to rows 2 and 3
+  return x;
 }
 __device__ __forceinline__ int lane_of(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
 __device__ __forceinline__ float lane_of(float v, int l) {
@@ -376,7 +383,8 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
   constexpr int GS = NT == 1 ? 4 : 2, ROWS = 16 * GS;
   constexpr int COLS = SHARE ? 16 * NT : 16 * NT * kPagesWaves;
   constexpr int OS = D + 4;  // row stride of a column's partial in LDS
-  __shared__ int64_t pre[kPagesThreads + 1];
+  __shared__ int wave_cost[kPagesWaves];
+  __shared__ Place begin;
   __shared__ Request reqs[kPagesThreads];  // all of them where there are no more than threads
   // two sets in turn: a wave writes a tile's while others still read the last one's
   __shared__ float joined[2][2][kPagesWaves][16 * NT];
@@ -388,86 +396,81 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
 
   // the call's work and this workgroup's share of it
   const int chunk = (a.n_req + kPagesThreads - 1) / kPagesThreads;
-  {
-    int64_t own = 0;
-    for (int r = tid * chunk; r < min((tid + 1) * chunk, a.n_req); ++r) {
-      const Request q = request_of(a, r);
-      reqs[tid] = q;
-      own += a.whole_tiles ? (q.m + tt - 1) / tt : request_cost(q, tt, a.causal);
-    }
-    int64_t inc = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t up = __shfl_up(inc, o);
-      if (lane >= o) inc += up;
-    }
-    if (lane == 63) pre[1 + tid] = inc;
-    __syncthreads();
-    int64_t before = 0;
-    for (int w = 0; w < wave; ++w) before += pre[64 * (w + 1)];
-    __syncthreads();
-    if (tid == 0) pre[0] = 0;
-    pre[1 + tid] = before + inc;
-    __syncthreads();
+  const auto get = [&](int r) {
+    const Request q = chunk == 1 ? reqs[r] : request_of(a, r);
+    return Request{q.start, q.m, q.n};
+  };
+  int own = 0;  // of this thread's requests
+  for (int r = tid * chunk; r < min((tid + 1) * chunk, a.n_req); ++r) {
+    const Request q = request_of(a, r);
+    if (chunk == 1) reqs[tid] = q;
+    const int all = tiles_of(q.m, tt, a.tt_inv);
+    own += a.whole_tiles ? all : tiles_cost(q, all, all, tt, a.causal);
   }
-  const int64_t X = uniform(H * pre[kPagesThreads]);
-  // (a share is at least kTileCost long, so none is empty)
-  if (a.whole_tiles && blockIdx.x >= X) return;
-  // As many shares as keep kLeastRows each, up to the grid; one for a tile where that is
+  own *= H;
+  int upto = wave_scan(own);
+  if (lane == 63) wave_cost[wave] = upto;
+  __syncthreads();
+  int X = 0;
+#pragma unroll
+  for (int k = 0; k < kPagesWaves; ++k) {
+    const int c = wave_cost[k];
+    if (k < wave) upto += c;
+    X += c;
+  }
+  X = uniform(X);
+  if (a.whole_tiles && (int)blockIdx.x >= X) return;
+  // As many shares as keep kLeastShare each, up to the grid; one for a tile where that is
   // about as many, so that tiles of like length are not cut.
-  int64_t want = X / kLeastRows;
-  if (want < 2 * a.least_tiles) want = a.least_tiles;
-  int W = (int)min(min((int64_t)gridDim.x, X / kTileCost), want);
+  int W = X / kLeastShare;
+  if (W < 2 * a.least_tiles) W = a.least_tiles;
+  W = min(min((int)gridDim.x, W), X / kTileCost);
   if (W >= kXcds) W -= W % kXcds;
-  const int64_t L = uniform(share_length(X, max(W, 1)));
+  W = max(W, 1);
+  const int L = uniform((int)((uint32_t)(X + W - 1) / (uint32_t)W));
   int4* meta = a.meta + blockIdx.x;
   // consecutive shares on one XCD, whose L2 then holds the rows that tiles share
   const int w = W >= kXcds ? (int)(blockIdx.x % kXcds) * (W / kXcds) + blockIdx.x / kXcds : blockIdx.x;
-  int64_t b0 = uniform(w * L), b1 = min(b0 + L, X);
+  int b0 = blockIdx.x, b1 = 0;
   if (!a.whole_tiles) {
     if (tid == 0) *meta = make_int4(-1, 0, 0, 0);
-    if ((int)blockIdx.x >= W || b0 >= X) return;
-  } else {
-    b0 = blockIdx.x;
+    if ((int)blockIdx.x >= W || w * (int64_t)L >= X) return;
+    b0 = w * L;
+    b1 = min(b0 + L, X);
   }
 
-  // the tile that b0 falls in
-  Place at;
-  const auto get = [&](int r) { return chunk == 1 ? reqs[r] : request_of(a, r); };
-  {
-    int lo = 0, hi = kPagesThreads;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (H * pre[mid] <= b0) lo = mid;
-      else hi = mid;
-    }
+  // The thread one of whose requests holds position b0 finds the tile.
+  if (b0 < upto && b0 >= upto - own) {
+    Place at;
     if (!a.whole_tiles) {
-      at = place_of(get, lo * chunk, H * pre[lo], b0, H, tt, a.causal);
+      at = place_of(get, tid * chunk, upto - own, b0, H, tt, a.tt_inv, a.causal);
     } else {  // a request's last tiles, which see most, first; its heads side by side
-      int x = (int)(b0 - H * pre[lo]), n_tiles;
-      for (at.r = lo * chunk;; ++at.r) {
+      int x = b0 - (upto - own);
+      for (at.r = tid * chunk;; ++at.r) {
         at.rq = get(at.r);
-        n_tiles = (at.rq.m + tt - 1) / tt;
-        if (x < H * n_tiles) break;
-        x -= H * n_tiles;
+        at.all = tiles_of(at.rq.m, tt, a.tt_inv);
+        if (x < H * at.all) break;
+        x -= H * at.all;
       }
       at.head = x % H;
-      at.tile = n_tiles - 1 - x / H;
-      at.p = b0 = 0;
-      b1 = kTileCost + seen_upto(at.rq, (at.tile + 1) * tt, a.causal);
+      at.tile = at.all - 1 - x / H;
+      at.head0 = at.cost = at.p0 = 0;
+      at.p1 = 1;  // the whole of what the workgroup does
     }
-    at = Place{uniform(at.r), uniform(at.head), uniform(at.tile), uniform(at.p),
-               Request{uniform(at.rq.start), uniform(at.rq.m), uniform(at.rq.n)}};
-    b0 = uniform(b0);
-    b1 = uniform(b1);
+    begin = at;
   }
+  __syncthreads();
+  Place at{uniform(begin.r), uniform(begin.head), uniform(begin.tile), uniform(begin.all), uniform(begin.p0),
+           uniform(begin.p1), uniform(begin.head0), uniform(begin.cost),
+           Request{uniform(begin.rq.start), uniform(begin.rq.m), uniform(begin.rq.n)}};
+  if (a.whole_tiles) b0 = 0, b1 = 1;
   bool first = true;
   int parity = 0;
-  for (int64_t pos = b0; pos < b1;) {
+  for (int pos = b0; pos < b1;) {
     const int j0 = uniform(at.tile * tt), ntok = uniform(min(tt, at.rq.m - at.tile * tt)), n = uniform(at.rq.n);
     const int req = uniform(at.r), g = uniform(at.head), start = uniform(at.rq.start), m = uniform(at.rq.m);
     const int vis_hi = uniform(seen_upto(at.rq, j0 + ntok, a.causal));
-    const int64_t p0 = uniform(at.p), p1 = p0 + kTileCost + vis_hi;
+    const int p0 = uniform(at.p0), p1 = uniform(at.p1);
     const int ra = uniform(row_at(b0, p0, p1, vis_hi)), rb = uniform(row_at(b1, p0, p1, vis_hi));
     const bool whole = b0 <= p0 && b1 >= p1;
     const int slot = 2 * w + (first ? 0 : 1);
@@ -631,12 +634,12 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
     }
     // a tile that begins here and goes on in the next workgroups: joined afterwards
     if (tid == 0 && b0 <= p0 && b1 < p1) {
-      const int we = (int)((p1 - 1) / L);
+      const int we = (p1 - 1) / L;
       *meta = make_int4((int)q0, ncol, slot, we);
     }
     first = false;
     pos = p1;
-    if (pos < b1) next_tile(get, at, p1, H, tt);
+    if (pos < b1) next_tile(get, at, H, tt, a.tt_inv, a.causal);
   }
 }
 
@@ -871,7 +874,11 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   const int64_t most = (int64_t)H * (n_tok / tt + std::min(n_req, n_tok));
   a.least_tiles = (int)std::min<int64_t>(kGrid, least);
   a.G_inv = (65536 + G - 1) / G;
-  a.whole_tiles = tiling != kFew && least >= kGrid / 2;
+  a.tt_inv = reciprocal(tt);
+  // Whole tiles where there are enough of them and each is long (a part's sums are as much
+  // again as 64 columns' rows), or where positions might not fit 31 bits.
+  const int64_t longest = kTileCost + ((int64_t)table_width * pages->page_tokens + kRowAlign - 1) / kRowAlign;
+  a.whole_tiles = (tiling != kFew && least >= kGrid / 2) || most * longest > INT32_MAX / 2;
   const int grid = a.whole_tiles ? (int)most : kGrid;
   if (d == 64) launch_pages<64>(a, tiling, grid, s);
   else launch_pages<128>(a, tiling, grid, s);

@@ -1,6 +1,7 @@
 // Checks the division of a paged attention call's work into shares (milo_pages.h) on the
 // host: over random batches every tile's rows are covered once, in order, by consecutive
 // shares, and the shares agree on who holds what.  Prints "ok <calls> <tiles> <split tiles>".
+#include <algorithm>
 #include <cstdio>
 #include <cstdlib>
 #include <random>
@@ -26,8 +27,14 @@ int main() {
   auto pick = [&](int lo, int hi) { return lo + (int)(rng() % (unsigned)(hi - lo + 1)); };
   long tiles_seen = 0, split = 0;
   int call = 0;
+  for (int tt = 1; tt <= 128; ++tt)
+    for (int k = 0; k < 2000; ++k) {
+      const int m = k < 500 ? k : pick(0, 1 << 24);
+      CHECK(tiles_of(m, tt, reciprocal(tt)) == (m + tt - 1) / tt);
+    }
   for (; call < 3000; ++call) {
-    const int n_req = pick(1, call % 3 ? 6 : 400), H = pick(1, 8), tt = pick(1, 256), causal = pick(0, 1);
+    const int n_req = pick(1, call % 3 ? 6 : 400), H = pick(1, 8), tt = pick(1, 128), causal = pick(0, 1);
+    const uint32_t inv = reciprocal(tt);
     const int long_n = call % 5 == 0 ? 100000 : 700, many = call % 4 == 0 ? 900 : 5;
     std::vector<Request> req(n_req);
     int start = 0;
@@ -45,46 +52,45 @@ int main() {
       }
       return req[r];
     };
-    std::vector<int64_t> pre(n_req + 1, 0);
+    std::vector<int> pre(n_req + 1, 0);
     for (int r = 0; r < n_req; ++r) {
       const int all = (req[r].m + tt - 1) / tt;
-      int64_t sum = 0;
-      for (int k = 0; k < all; ++k) {
-        CHECK(tiles_cost(req[r], k, tt, causal) == sum);
-        sum += kTileCost + seen_upto(req[r], (k + 1) * tt, causal);
+      int64_t rows = 0;
+      for (int k = 0; k <= all; ++k) {
+        CHECK(tiles_cost(req[r], k, all, tt, causal) == rows / kRowAlign + k * kTileCost);
+        if (k < all) rows += seen_upto(req[r], (k + 1) * tt, causal);
       }
-      CHECK(request_cost(req[r], tt, causal) == sum);
-      pre[r + 1] = pre[r] + H * sum;
+      const int64_t next = pre[r] + (int64_t)H * tiles_cost(req[r], all, all, tt, causal);
+      CHECK(next < INT32_MAX);
+      pre[r + 1] = (int)next;
     }
-    const int64_t X = pre[n_req];
+    const int X = pre[n_req];
     if (X == 0) continue;
-    const int W = (int)std::min<int64_t>(pick(1, 512), X);
+    const int W = std::min(pick(1, 512), X), L = (X + W - 1) / W;
     // the tiles in order, each with the row up to which it is done
     int r = 0, head = 0, tile = 0, done = 0, parts = 0, last_end = -1;
     while (req[r].m == 0) ++r;
-    const int64_t L = share_length(X, W);
-    CHECK((X + L - 1) / L <= W);
     for (int w = 0; w < W; ++w) {
-      const int64_t b0 = w * L, b1 = std::min(b0 + L, X);
+      const int b0 = w * L, b1 = std::min(b0 + L, X);
       if (b0 >= X) continue;
       int lo = 0;
       while (pre[lo + 1] <= b0) ++lo;
       lo = lo > 2 ? lo - pick(0, 2) : lo;  // any request before will do
-      Place at = place_of(get, lo, pre[lo], b0, H, tt, causal);
+      Place at = place_of(get, lo, pre[lo], b0, H, tt, inv, causal);
       bool first = true;
-      for (int64_t pos = b0; pos < b1;) {
+      for (int pos = b0; pos < b1;) {
         CHECK(calls_out == 0 && at.r == r && at.head == head && at.tile == tile);
         const Request q = at.rq;
         const int j0 = tile * tt, ntok = std::min(tt, q.m - j0), vis = seen_upto(q, j0 + ntok, causal);
         CHECK(ntok >= 1 && vis <= q.n);
-        const int64_t p0 = at.p, p1 = p0 + kTileCost + vis;
+        const int p0 = at.p0, p1 = at.p1;
         CHECK(p0 <= pos && pos < p1 && (first || p0 == pos));
         const int ra = row_at(b0, p0, p1, vis), rb = row_at(b1, p0, p1, vis);
-        CHECK(ra == done && ra <= rb && rb <= vis && (ra % kRowAlign == 0 || ra == vis));
+        CHECK(ra == done && ra <= rb && rb <= vis && (ra % kRowAlign == 0 || ra == vis) && (rb % kRowAlign == 0 || rb == vis));
         CHECK(pos / L == w && (std::min(p1, b1) - 1) / L == w);
         const bool whole = b0 <= p0 && b1 >= p1;
         CHECK(!whole || (ra == 0 && rb == vis && parts == 0));
-        if (!whole && b0 <= p0) last_end = (int)((p1 - 1) / L);
+        if (!whole && b0 <= p0) last_end = (p1 - 1) / L;
         if (!whole) CHECK(parts == 0 ? b0 <= p0 && b1 < p1 : first);
         done = rb;
         ++parts;
@@ -104,7 +110,7 @@ int main() {
           }
         }
         first = false;
-        if (pos < b1) next_tile(get, at, p1, H, tt);
+        if (pos < b1) next_tile(get, at, H, tt, inv, causal);
       }
     }
     CHECK(r == n_req && calls_out == 0);
