@@ -41,15 +41,31 @@ struct PlanArgs {
   int32_t n_req, lg_page, width, n_pages, n_slots;
 };
 
+// Sums that stop at 2^32 - 1, past every limit they are held against.
 struct Sums {
-  int64_t rows, taken, given;
+  uint32_t rows, taken, given;
 };
 
-__device__ inline Sums add(Sums a, Sums b) { return {a.rows + b.rows, a.taken + b.taken, a.given + b.given}; }
+__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+__device__ __forceinline__ Sums add(Sums a, Sums b) {
+  return {sat_add(a.rows, b.rows), sat_add(a.taken, b.taken), sat_add(a.given, b.given)};
+}
+// sums over the lanes up to this one
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+#define MILO_FROM(ctrl, rows) x = sat_add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xF, false))
+  MILO_FROM(0x111, 0xF);  // 1, 2, 4, 8 lanes before, in rows of 16
+  MILO_FROM(0x112, 0xF);
+  MILO_FROM(0x114, 0xF);
+  MILO_FROM(0x118, 0xF);
+  MILO_FROM(0x142, 0xA);  // rows 0 and 2 to rows 1 and 3
+  MILO_FROM(0x143, 0xC);  // row 1 to rows 2 and 3
+#undef MILO_FROM
+  return x;
+}
 
-// what request i adds to the sums; *flags: what is wrong with it
-__device__ inline Sums plan_one(const PlanArgs& a, int i, int* flags) {
-  const int64_t n = a.lens[i], m = n + a.delta[i], cap = (int64_t)a.width << a.lg_page;
+// what a request of n rows and change delta adds to the sums; *flags: what is wrong with it
+__device__ inline Sums plan_one(const PlanArgs& a, int n, int delta, int* flags) {
+  const int64_t m = (int64_t)n + delta, cap = (int64_t)a.width << a.lg_page;
   if (n < 0 || m < 0) {
     *flags |= kBadLength;
     return {0, 0, 0};
@@ -58,108 +74,19 @@ __device__ inline Sums plan_one(const PlanArgs& a, int i, int* flags) {
     *flags |= kRowNarrow;
     return {0, 0, 0};
   }
-  const int64_t r = (1 << a.lg_page) - 1, p0 = (n + r) >> a.lg_page, p1 = (m + r) >> a.lg_page;
-  return {m > n ? m - n : 0, p1 > p0 ? p1 - p0 : 0, p0 > p1 ? p0 - p1 : 0};
+  const int r = (1 << a.lg_page) - 1, p0 = (int)(((int64_t)n + r) >> a.lg_page), p1 = (int)((m + r) >> a.lg_page);
+  return {(uint32_t)max(delta, 0), (uint32_t)max(p1 - p0, 0), (uint32_t)max(p0 - p1, 0)};
 }
+
+// x < 2 n_pages as an index of the ring
+__device__ inline int ring_at(const PlanArgs& a, int64_t x) { return (int)(x >= a.n_pages ? x - a.n_pages : x); }
 
 // the slot of packed new row x, which is row `row` of request i, whose first `held` pages
 // are in the table and whose others are the ring's from the taken-th on
 __device__ inline int slot_at(const PlanArgs& a, int i, int row, int held, int taken, int head) {
   const int pg = row >> a.lg_page, P = 1 << a.lg_page;
-  const int id = pg < held ? a.table[(int64_t)i * a.width + pg] : a.ring[((int64_t)head + taken + pg - held) % a.n_pages];
+  const int id = pg < held ? a.table[(int64_t)i * a.width + pg] : a.ring[ring_at(a, (int64_t)head + taken + pg - held)];
   return (uint32_t)id < (uint32_t)a.n_pages ? (id << a.lg_page) + (row & (P - 1)) : -1;
-}
-
-__device__ inline int owner_of(const int32_t* first, int n, int x);
-
-// FILL: n_req <= kPlanThreads; the workgroup also writes slots and pages, the sums in
-// LDS, so that a decode step's plan is one launch.
-template <bool FILL>
-__global__ __launch_bounds__(kPlanThreads) void plan_scan_kernel(PlanArgs a) {
-  __shared__ int first[FILL ? 4 : 1][FILL ? kPlanThreads : 1];  // starts, taken, given, length before
-  __shared__ Sums wave_sum[kPlanThreads / 64];
-  __shared__ int all_flags;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (tid == 0) all_flags = 0;
-  Sums carry{0, 0, 0};
-  int flags = 0;
-  for (int base = 0; base < a.n_req; base += kPlanThreads) {
-    const int i = base + tid;
-    const Sums own = i < a.n_req ? plan_one(a, i, &flags) : Sums{0, 0, 0};
-    Sums inc = own;
-    for (int o = 1; o < 64; o <<= 1) {
-      const Sums up{__shfl_up(inc.rows, o), __shfl_up(inc.taken, o), __shfl_up(inc.given, o)};
-      if (lane >= o) inc = add(inc, up);
-    }
-    __syncthreads();  // the last round's sums have been read
-    if (lane == 63) wave_sum[wave] = inc;
-    __syncthreads();
-    Sums before = carry;
-    for (int w = 0; w < wave; ++w) before = add(before, wave_sum[w]);
-    for (int w = 0; w < kPlanThreads / 64; ++w) carry = add(carry, wave_sum[w]);
-    if (i < a.n_req) {
-      // sums past 2^31 are cut: such a step is stopped below and they are not used
-      const Sums at{before.rows + inc.rows - own.rows, before.taken + inc.taken - own.taken,
-                    before.given + inc.given - own.given};
-      a.starts[i] = (int32_t)at.rows;
-      if constexpr (FILL) {
-        first[0][i] = (int32_t)at.rows;
-        first[1][i] = (int32_t)at.taken;
-        first[2][i] = (int32_t)at.given;
-        first[3][i] = a.lens[i];
-      } else {
-        a.taken[i] = (int32_t)at.taken;
-        a.given[i] = (int32_t)at.given;
-      }
-    }
-  }
-  __syncthreads();
-  if (flags) atomicOr(&all_flags, flags);
-  __syncthreads();
-  flags = all_flags;
-  const int64_t head = a.ring_state[0], count = a.ring_state[1], n = a.n_pages;
-  if (head < 0 || head >= n || count < 0 || count > n || count + carry.given > n) flags |= kBadRing;
-  else if (carry.taken > count) flags |= kPoolShort;
-  if (carry.rows > a.n_slots) flags |= kSlotsShort;
-  for (int i = tid; i < a.n_req; i += kPlanThreads) {
-    a.lens_out[i] = a.lens[i] + (flags ? 0 : a.delta[i]);
-    if (flags) a.starts[i] = 0;
-  }
-  __syncthreads();  // ring_state is read by every thread before it may be written
-  if (tid == 0) {
-    a.starts[a.n_req] = flags ? 0 : (int32_t)carry.rows;
-    a.ring_state_out[0] = (int32_t)(flags ? head : (head + carry.taken) % n);
-    a.ring_state_out[1] = (int32_t)(flags ? count : count - carry.taken + carry.given);
-    a.status[0] = flags;
-    if constexpr (!FILL) {
-      a.total[0] = flags ? 0 : (int32_t)carry.taken;
-      a.total[1] = flags ? 0 : (int32_t)carry.given;
-      a.total[3] = (int32_t)head;
-      a.total[4] = (int32_t)count;
-      a.total[5] = flags ? 0 : (int32_t)carry.rows;
-    }
-  }
-  if constexpr (FILL) {
-    const int rows = flags ? 0 : (int)carry.rows, taken = flags ? 0 : (int)carry.taken, given = flags ? 0 : (int)carry.given;
-    const int P = 1 << a.lg_page, items = a.n_slots + taken + given;
-    for (int x = tid; x < items; x += kPlanThreads) {
-      if (x < a.n_slots) {
-        int slot = -1;
-        if (x < rows) {
-          const int i = owner_of(first[0], a.n_req, x), n = first[3][i];
-          slot = slot_at(a, i, n + x - first[0][i], (n + P - 1) >> a.lg_page, first[1][i], (int)head);
-        }
-        a.slots[x] = slot;
-      } else if (x < a.n_slots + taken) {
-        const int y = x - a.n_slots, i = owner_of(first[1], a.n_req, y), held = (first[3][i] + P - 1) >> a.lg_page;
-        a.table[(int64_t)i * a.width + held + y - first[1][i]] = a.ring[(head + y) % a.n_pages];
-      } else {
-        const int y = x - a.n_slots - taken, i = owner_of(first[2], a.n_req, y);
-        const int kept = (first[3][i] + a.delta[i] + P - 1) >> a.lg_page;
-        a.ring[(head + count + y) % a.n_pages] = a.table[(int64_t)i * a.width + kept + y - first[2][i]];
-      }
-    }
-  }
 }
 
 // the last i with first[i] <= x (first[0] = 0 <= x, not decreasing)
@@ -171,6 +98,103 @@ __device__ inline int owner_of(const int32_t* first, int n, int x) {
     else hi = mid;
   }
   return lo;
+}
+
+// FILL: n_req <= kPlanThreads; the workgroup also writes slots and pages, the sums in
+// LDS, so that a decode step's plan is one launch.
+template <bool FILL>
+__global__ __launch_bounds__(kPlanThreads) void plan_scan_kernel(PlanArgs a) {
+  constexpr int kPlanWaves = kPlanThreads / 64;
+  __shared__ int first[FILL ? 4 : 1][FILL ? kPlanThreads : 1];  // starts, taken, given, length before
+  __shared__ Sums wave_sum[kPlanWaves];
+  __shared__ int all_flags;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int head = a.ring_state[0], count = a.ring_state[1];
+  if (tid == 0) all_flags = 0;
+  Sums carry{0, 0, 0};
+  int flags = 0;
+  for (int base = 0; base < a.n_req; base += kPlanThreads) {
+    const int i = base + tid;
+    const int n = i < a.n_req ? a.lens[i] : 0, delta = i < a.n_req ? a.delta[i] : 0;
+    const Sums own = plan_one(a, n, delta, &flags);
+    const Sums inc{wave_scan(own.rows), wave_scan(own.taken), wave_scan(own.given)};
+    __syncthreads();  // the last round's sums have been read
+    if (lane == 63) wave_sum[wave] = inc;
+    __syncthreads();
+    Sums before = carry;
+#pragma unroll
+    for (int w = 0; w < kPlanWaves; ++w) {
+      const Sums s = wave_sum[w];
+      if (w < wave) before = add(before, s);
+      carry = add(carry, s);
+    }
+    if (i < a.n_req) {
+      // (sums that stopped are not used: the step is refused below)
+      const Sums at{before.rows + inc.rows - own.rows, before.taken + inc.taken - own.taken,
+                    before.given + inc.given - own.given};
+      if constexpr (FILL) {
+        first[0][i] = (int32_t)at.rows;
+        first[1][i] = (int32_t)at.taken;
+        first[2][i] = (int32_t)at.given;
+        first[3][i] = n;
+      } else {
+        a.starts[i] = (int32_t)at.rows;
+        a.taken[i] = (int32_t)at.taken;
+        a.given[i] = (int32_t)at.given;
+      }
+    }
+  }
+  if (flags) atomicOr(&all_flags, flags);
+  __syncthreads();
+  flags = all_flags;
+  if (head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages || carry.given > (uint32_t)(a.n_pages - count))
+    flags |= kBadRing;
+  else if (carry.taken > (uint32_t)count)
+    flags |= kPoolShort;
+  if (carry.rows > (uint32_t)a.n_slots) flags |= kSlotsShort;
+  const int rows = flags ? 0 : (int)carry.rows, taken = flags ? 0 : (int)carry.taken, given = flags ? 0 : (int)carry.given;
+  for (int i = tid; i < a.n_req; i += kPlanThreads) {
+    if constexpr (FILL) {
+      a.starts[i] = flags ? 0 : first[0][i];
+      a.lens_out[i] = first[3][i] + (flags ? 0 : a.delta[i]);
+    } else {
+      if (flags) a.starts[i] = 0;
+      a.lens_out[i] = a.lens[i] + (flags ? 0 : a.delta[i]);
+    }
+  }
+  if (tid == 0) {  // every thread has read ring_state, which this may be, before the barriers above
+    a.starts[a.n_req] = rows;
+    a.ring_state_out[0] = flags ? head : ring_at(a, (int64_t)head + taken);
+    a.ring_state_out[1] = count - taken + given;
+    a.status[0] = flags;
+    if constexpr (!FILL) {
+      a.total[0] = taken;
+      a.total[1] = given;
+      a.total[3] = head;
+      a.total[4] = count;
+      a.total[5] = rows;
+    }
+  }
+  if constexpr (FILL) {
+    const int P = 1 << a.lg_page, items = a.n_slots + taken + given;
+    for (int x = tid; x < items; x += kPlanThreads) {
+      if (x < a.n_slots) {
+        int slot = -1;
+        if (x < rows) {
+          const int i = owner_of(first[0], a.n_req, x), n = first[3][i];
+          slot = slot_at(a, i, n + x - first[0][i], (n + P - 1) >> a.lg_page, first[1][i], head);
+        }
+        a.slots[x] = slot;
+      } else if (x < a.n_slots + taken) {
+        const int y = x - a.n_slots, i = owner_of(first[1], a.n_req, y), held = (first[3][i] + P - 1) >> a.lg_page;
+        a.table[(int64_t)i * a.width + held + y - first[1][i]] = a.ring[ring_at(a, (int64_t)head + y)];
+      } else {
+        const int y = x - a.n_slots - taken, i = owner_of(first[2], a.n_req, y);
+        const int kept = (first[3][i] + a.delta[i] + P - 1) >> a.lg_page;
+        a.ring[ring_at(a, (int64_t)head + count + y)] = a.table[(int64_t)i * a.width + kept + y - first[2][i]];
+      }
+    }
+  }
 }
 
 __global__ __launch_bounds__(kFillThreads) void plan_fill_kernel(PlanArgs a) {
@@ -189,11 +213,11 @@ __global__ __launch_bounds__(kFillThreads) void plan_fill_kernel(PlanArgs a) {
     } else if (x < (int64_t)a.n_slots + taken) {
       const int y = (int)(x - a.n_slots), i = owner_of(a.taken, a.n_req, y);
       const int held = (a.lens_out[i] - a.delta[i] + P - 1) >> a.lg_page;
-      a.table[(int64_t)i * a.width + held + y - a.taken[i]] = a.ring[((int64_t)head + y) % a.n_pages];
+      a.table[(int64_t)i * a.width + held + y - a.taken[i]] = a.ring[ring_at(a, (int64_t)head + y)];
     } else {
       const int y = (int)(x - a.n_slots - taken), i = owner_of(a.given, a.n_req, y);
       const int kept = (a.lens_out[i] + P - 1) >> a.lg_page;
-      a.ring[((int64_t)head + count + y) % a.n_pages] = a.table[(int64_t)i * a.width + kept + y - a.given[i]];
+      a.ring[ring_at(a, (int64_t)head + count + y)] = a.table[(int64_t)i * a.width + kept + y - a.given[i]];
     }
   }
 }

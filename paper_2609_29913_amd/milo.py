@@ -6,11 +6,13 @@ the library is required - there is no fallback, and a missing library raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Sequence
 
 import numpy as np
+import torch  # also loads the HIP runtime that libmilo.so binds to (lib)
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmilo.so")
 
@@ -62,10 +64,9 @@ def lib() -> ctypes.CDLL:
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is not built: run __graft_entry__.build()")
-        # PyTorch ships its own HIP runtime; loading it first makes the library
+        # PyTorch ships its own HIP runtime; having it loaded makes the library
         # bind to that same runtime (one runtime per process), so torch tensors
         # and streams can be passed across the boundary
-        import torch  # noqa: F401
         L = ctypes.CDLL(LIB_PATH)
         vp = ctypes.c_void_p
         L.milo_cache_create.argtypes = [ctypes.POINTER(milo_cache_desc), ctypes.POINTER(vp),
@@ -169,7 +170,6 @@ def _dev_tensor(x, name: str, dtypes, ndim: int | None = None):
     """Require a contiguous tensor on the current GPU with one of `dtypes`
     (names), so that no host pointer, wrong element type or strided view ever
     reaches a kernel."""
-    import torch
     if not isinstance(x, torch.Tensor):
         raise ValueError(f"{name} must be a torch tensor on the GPU, got {type(x).__name__}")
     if not x.is_cuda:
@@ -209,7 +209,6 @@ def _i32(seq) -> _I32Arg | None:
 def _stream(stream) -> int:
     if stream is not None:
         return stream if isinstance(stream, int) else int(stream.cuda_stream)
-    import torch
     return int(torch.cuda.current_stream().cuda_stream)
 
 
@@ -350,7 +349,6 @@ def milo_allocate_ranks(sigma, n_sv, r_total: int, r_min: int, r_max: int, strea
     """Per-block ranks (Sec. 4.3 allocation).  sigma: device fp32 [n_blocks][ld]
     tensor of non-increasing singular values, n_sv: host [n_blocks] counts.
     Returns int32 [n_blocks]; synchronous."""
-    import torch
     if not isinstance(sigma, torch.Tensor) or not sigma.is_cuda or sigma.dtype != torch.float32 \
             or sigma.dim() != 2 or sigma.stride(1) != 1:
         raise ValueError("sigma must be a float32 GPU tensor [n_blocks][ld] with unit column stride")
@@ -382,7 +380,6 @@ def milo_block_svd(blocks, stream=None):
     every block.  blocks: list of device bf16 tensors [T_b][D] (one shared D).
     Returns (sigma float32 [n_blocks][D], vt float32 [n_blocks][D][D]) on the
     GPU; synchronous."""
-    import torch
     if not blocks:
         raise ValueError("no blocks")
     D = int(blocks[0].shape[1])
@@ -411,7 +408,6 @@ def milo_block_svd_flops() -> float:
 def milo_block_factors(blocks, vt, ranks, stream=None):
     """The truncated factors P_b = K_b V_r (bf16 [T_b][r_b]) and R_b = V_r^T
     (bf16 [r_b][D]) of every block, as device int16 tensors of bf16 bits."""
-    import torch
     D = int(blocks[0].shape[1])
     ptrs = _dev_ptrs(blocks, "blocks", D)
     if tuple(vt.shape) != (len(blocks), D, D) or vt.dtype != torch.float32 or not vt.is_cuda or \
@@ -440,7 +436,6 @@ class MiloPages:
     this object."""
 
     def __init__(self, k_codes, v_codes, k_scale, v_scale, page_tokens: int):
-        import torch
         fmt = {torch.int8: MILO_KV_INT8, torch.float8_e4m3fn: MILO_KV_E4M3}
         for name, x in (("k_codes", k_codes), ("v_codes", v_codes)):
             if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in fmt or x.dim() != 3 or \
@@ -467,7 +462,6 @@ class MiloPages:
 def milo_pages_create(n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int, fmt: int = MILO_KV_INT8,
                       device=None) -> MiloPages:
     """A zeroed pool on the GPU (fmt: MILO_KV_INT8 or MILO_KV_E4M3)."""
-    import torch
     if fmt not in (MILO_KV_INT8, MILO_KV_E4M3):
         raise ValueError(f"fmt must be MILO_KV_INT8 or MILO_KV_E4M3, got {fmt}")
     dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
@@ -482,7 +476,6 @@ def milo_pages_create(n_pages: int, page_tokens: int, n_kv_heads: int, head_dim:
 # comparison per property, messages only where one fails.
 
 def _pages_arg(pages) -> MiloPages:
-    import torch
     if not isinstance(pages, MiloPages):
         raise ValueError(f"pages must be a MiloPages, got {type(pages).__name__}")
     if pages.device.index != torch.cuda.current_device():
@@ -492,21 +485,16 @@ def _pages_arg(pages) -> MiloPages:
 
 def _i32_dev(x, name: str, dev: int, *shape: int):
     """A contiguous int32 tensor on GPU `dev` of the given shape (-1: any)."""
-    import torch
     if not isinstance(x, torch.Tensor) or x.dtype is not torch.int32 or x.get_device() != dev or not x.is_contiguous():
         _dev_tensor(x, name, ("torch.int32",))
     got = x.shape
-    if len(got) != len(shape):
-        raise ValueError(f"{name} must have {len(shape)} dimensions, got shape {tuple(got)}")
-    for w, n in zip(shape, got):
-        if w != n and w >= 0:
-            raise ValueError(f"{name} has shape {tuple(got)}, expected {tuple(shape)}")
+    if len(got) != len(shape) or (shape[0] != got[0] and shape[0] >= 0):
+        raise ValueError(f"{name} has shape {tuple(got)}, expected {tuple(shape)}")
     return x
 
 
 def _row_stride(x, name: str, dev: int, heads: int, d: int) -> int:
     """Row stride (elements) of bf16 rows [n][heads][d] whose rows may lie apart."""
-    import torch
     if not isinstance(x, torch.Tensor) or x.get_device() != dev:
         raise ValueError(f"{name} must be a tensor on the current GPU (cuda:{dev})")
     if x.dtype is not torch.bfloat16 and str(x.dtype) not in _BF16_DTYPES:
@@ -522,21 +510,20 @@ def _row_stride(x, name: str, dev: int, heads: int, d: int) -> int:
     return row if shape[0] > 1 else heads * d
 
 
+# the current stream's handle by torch's short way, where it has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_on(stream, dev: int) -> int:
-    """Handle of `stream` (None: the current one of GPU `dev`, by torch's short way where it has it)."""
-    import torch
-    if stream is None:
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return raw(dev) if raw is not None else _stream(None)
+    """Handle of `stream` (None: the current one of GPU `dev`)."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
     return _stream(stream)
 
 
 def _on_stream(stream):
     """A context in which torch allocates on `stream` (None: as it is), so that memory made
     for a call is neither still in use by, nor handed on to, another stream's work."""
-    import contextlib
-
-    import torch
     if stream is None:
         return contextlib.nullcontext()
     if isinstance(stream, int):
@@ -553,7 +540,6 @@ def milo_pages_plan(lens, delta, page_tokens: int, table, ring, ring_state, n_sl
     ring_state [2] (head, count).  Returns (lens_out, starts, slots, ring_state_out, status),
     made here where not given; slots has n_slots entries.  work: int32 tensor of at least
     milo_pages_plan_work(n_req) bytes, or None."""
-    import torch
     if not isinstance(lens, torch.Tensor) or not lens.is_cuda or lens.dim() != 1:
         raise ValueError("lens must be an int32 GPU tensor [n_req]")
     n_req, dev = lens.shape[0], torch.cuda.current_device()
@@ -629,7 +615,6 @@ def milo_attend_pages(pages: MiloPages, page_table, lens, q, scale: float, out, 
     are its last rows; False: every query sees all of them.  cache and block_table add selected
     blocks of a compressed context to every query's keys.  work: uint8 tensor of at least
     milo_attend_pages_work(...) bytes, or None."""
-    import torch
     p = _pages_arg(pages)
     dev = p.device.index
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
