@@ -238,7 +238,8 @@ struct StoreArgs {
   int64_t k_stride, v_stride;
   const int32_t* slots;
   int32_t n_tok, lg_page, n_slots;
-  int32_t chunk;  // rows of the call a wave looks at
+  int32_t chunk;  // rows of the call a workgroup looks at
+  int32_t share;  // waves that share a page's rows: 1 or 4 (all: they meet at a barrier)
 };
 
 __device__ inline uint32_t wave_max(uint32_t x) {
@@ -291,13 +292,16 @@ __device__ __forceinline__ uint32_t gather_byte(uint32_t a, uint32_t b, uint32_t
 }
 
 // rows x .. (run of them) into offsets off .. of a page and head: keys (VALUES false)
-// or values
+// or values.  `share` waves, this one `mine`, take its groups in turn and their largest
+// magnitudes together through `seen`.
 template <int D, int FMT, bool VALUES>
-__device__ void store_side(const uint16_t* x, int64_t stride, uint8_t* codes, float* scale_at, int off, int run) {
+__device__ void store_side(const uint16_t* x, int64_t stride, uint8_t* codes, float* scale_at, int off, int run, int mine,
+                           int share, uint32_t* seen, bool works) {
   constexpr int LPG = D / 2, GPW = 64 / LPG;  // lanes of a group of 16 rows, groups of a wave
-  const int lane = threadIdx.x & 63, sub = lane / LPG, ch = lane % (D / 8), q = lane % LPG / (D / 8);
-  const float was = off > 0 ? *scale_at : 0.f;
-  const int g0 = off >> 4, g1 = (off + run + 15) >> 4;
+  const int lane = threadIdx.x & 63, sub = mine * GPW + lane / LPG, step = share * GPW;
+  const int ch = lane % (D / 8), q = lane % LPG / (D / 8);
+  const float was = works && off > 0 ? *scale_at : 0.f;
+  const int g0 = off >> 4, g1 = works ? (off + run + 15) >> 4 : 0;
   uint4 v[4];
   const auto load = [&](int g) {  // the group's new rows, zeros in the others
 #pragma unroll
@@ -307,20 +311,27 @@ __device__ void store_side(const uint16_t* x, int64_t stride, uint8_t* codes, fl
     }
   };
   uint32_t mx = 0;
-  for (int g = g0 + sub; g < g1; g += GPW) {
+  for (int g = g0 + sub; g < g1; g += step) {
     load(g);
 #pragma unroll
     for (int i = 0; i < 4; ++i) mx = abs_max2(abs_max2(abs_max2(abs_max2(mx, v[i].x), v[i].y), v[i].z), v[i].w);
   }
-  float s = scale_of<FMT>(wave_max(max(mx & 0xFFFFu, mx >> 16)));
+  mx = wave_max(max(mx & 0xFFFFu, mx >> 16));
+  if (share > 1) {
+    if (lane == 0) seen[threadIdx.x >> 6] = mx;
+    __syncthreads();
+    for (int k = 0; k < share; ++k) mx = max(mx, seen[(threadIdx.x >> 6) - mine + k]);
+  }
+  if (!works) return;
+  float s = scale_of<FMT>(mx);
   if (off > 0 && !(s >= was)) s = was >= s || was != was ? was : s;  // the larger, NaN before all
   const bool grew = off > 0 && s != was && s == s;
-  const bool loaded = g1 - g0 <= GPW;  // the new rows are still in registers
-  for (int g = (grew ? 0 : g0) + sub; g < g1; g += GPW) {
-    if (g >= g0 && !(loaded && g - sub == g0)) load(g);
+  const bool loaded = g1 - g0 <= step;  // the new rows are still in registers
+  for (int g = grew ? (g0 + sub) % step : g0 + sub; g < g1; g += step) {
+    if (g >= g0 && !loaded) load(g);
     uint2 c[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = codes_of_row<FMT>(v[i], s);
+    for (int i = 0; i < 4; ++i) c[i] = g < g0 ? make_uint2(0, 0) : codes_of_row<FMT>(v[i], s);
     const int t0 = 16 * g + 4 * q;
     if constexpr (!VALUES) {
 #pragma unroll
@@ -358,23 +369,31 @@ __device__ void store_side(const uint16_t* x, int64_t stride, uint8_t* codes, fl
       }
     }
   }
-  if (lane == 0) *scale_at = s;
+  if (lane == 0 && mine == 0) *scale_at = s;
 }
 
-// Waves: `chunk` rows of the call by 2 H (head, side) pairs.  A row that begins a run
-// (rows that follow one another in a page) does it whole; the others are passed over.
+// Workgroups: `chunk` rows of the call by 4 / share of the 2 H (head, side) pairs.  A row
+// that begins a run (rows that follow one another in a page) brings the run with it; the
+// others are passed over.  All four waves go through the same runs.
 template <int D, int FMT>
 __global__ __launch_bounds__(kRowThreads) void store_kernel(StoreArgs a) {
+  __shared__ uint32_t seen[2][kRowThreads / 64];  // in turn: a wave may still read the last run's
   const int H = a.p.n_kv_heads, P = 1 << a.lg_page, lane = threadIdx.x & 63;
-  const int pair = blockIdx.y * (kRowThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (pair >= 2 * H) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave & (a.share - 1);
+  const int pair = (blockIdx.y * (kRowThreads / 64) + wave) / a.share;
+  const bool works = pair < 2 * H;
   const int h = pair >> 1;
-  const int64_t t1 = min((int64_t)a.n_tok, ((int64_t)blockIdx.x + 1) * a.chunk);
-  for (int64_t t = (int64_t)blockIdx.x * a.chunk; t < t1; ++t) {
-    const int slot = __builtin_amdgcn_readfirstlane(a.slots[t]);
-    if ((uint32_t)slot >= (uint32_t)a.n_slots) continue;
-    const int off = slot & (P - 1);
-    if (off > 0 && t > 0 && a.slots[t - 1] == slot - 1) continue;
+  int turn = 0;
+  // the rows that begin a run, by one look at the chunk's slots
+  const int64_t t0 = (int64_t)blockIdx.x * a.chunk, tl = t0 + lane;
+  const bool mine_to_see = lane < a.chunk && tl < a.n_tok;
+  const int slot_l = mine_to_see ? a.slots[tl] : -1, last_l = mine_to_see && tl > 0 ? a.slots[tl - 1] : -1;
+  const bool in = (uint32_t)slot_l < (uint32_t)a.n_slots;
+  uint64_t begins = __ballot(in && ((slot_l & (P - 1)) == 0 || tl == 0 || last_l != slot_l - 1));
+  for (; begins; begins &= begins - 1) {
+    const int l = __builtin_ctzll(begins);
+    const int64_t t = t0 + l;
+    const int slot = __builtin_amdgcn_readlane(slot_l, l), off = slot & (P - 1);
     int run = 0;  // rows whose slots go on from this one's in the page
     for (int k = 0; k < P; k += 64) {
       const int r = k + lane;
@@ -383,13 +402,14 @@ __global__ __launch_bounds__(kRowThreads) void store_kernel(StoreArgs a) {
       run += ~m == 0 ? 64 : __builtin_ctzll(~m);
       if (~m != 0) break;
     }
-    const int64_t ph = (int64_t)(slot >> a.lg_page) * H + h;
+    const int64_t ph = (int64_t)(slot >> a.lg_page) * H + (works ? h : 0);
     if (pair & 1)
       store_side<D, FMT, true>(a.v + t * a.v_stride + h * D, a.v_stride, (uint8_t*)a.p.v_codes + ph * P * D,
-                               a.p.v_scale + ph, off, run);
+                               a.p.v_scale + ph, off, run, mine, a.share, seen[turn], works);
     else
       store_side<D, FMT, false>(a.k + t * a.k_stride + h * D, a.k_stride, (uint8_t*)a.p.k_codes + ph * P * D,
-                                a.p.k_scale + ph, off, run);
+                                a.p.k_scale + ph, off, run, mine, a.share, seen[turn], works);
+    turn ^= 1;
   }
 }
 
@@ -582,10 +602,13 @@ int milo_pages_store(const milo_pages* pages, const uint16_t* k, int64_t k_strid
   a.n_tok = n_tok;
   a.lg_page = log2_page(pages->page_tokens);
   a.n_slots = pages->n_pages * pages->page_tokens;
-  // Few rows: a wave for each, since each may begin a run; many: a wave for 16 of them,
-  // most of which are inside another's run.
+  // Few rows: a workgroup for each, since each may begin a run; many: one for 16 of them,
+  // most of which are inside another's run.  The four waves share a page's rows where it has
+  // groups for them (4096 rows, pages of 64, 7B heads: 15.6 us with one wave each).
   a.chunk = n_tok <= 2048 ? 1 : 16;
-  const dim3 grid((n_tok + a.chunk - 1) / a.chunk, (2 * pages->n_kv_heads + 3) / 4);
+  const int groups = pages->page_tokens / (pages->head_dim == 64 ? 32 : 16);
+  a.share = groups >= 4 ? 4 : 1;
+  const dim3 grid((n_tok + a.chunk - 1) / a.chunk, (2 * pages->n_kv_heads * a.share + 3) / 4);
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   MILO_PAGES_DISPATCH(store_kernel, a, grid, kRowThreads, s);
   return launched("store kernel");
