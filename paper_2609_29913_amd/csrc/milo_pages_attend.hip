@@ -274,6 +274,8 @@ template <bool MASKED, int D, int FMT, int PARTS, int NT, int GS>
 __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&qf)[NT][D / 32], int row,
                                          int n, const int (&vis)[NT], Running<D, NT>& run) {
   const int lane = threadIdx.x & 63, q4 = (lane >> 4) * 4;
+  // products first where two waves compete: the other's arithmetic fills the gaps (5%)
+  __builtin_amdgcn_s_setprio(1);
   // two groups at a time: as many independent sums as hide a product's latency
   f32x4 s[GS][NT];
 #pragma unroll
@@ -295,6 +297,7 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
         }
     __builtin_amdgcn_sched_barrier(0);
   }
+  __builtin_amdgcn_s_setprio(0);
   // the conversions of the phases stay in them: moved up, they cost registers (spills)
   __builtin_amdgcn_sched_barrier(0);
   // exponents of the weights, relative to m (0 before any row)
@@ -347,6 +350,7 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
       run.l[t] = fmaf(sum, MASKED ? fabsf(st.rv[g]) : st.rv[g], run.l[t]);
     }
   }
+  __builtin_amdgcn_s_setprio(1);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int g = 0; g < GS; g += 2) {
@@ -374,6 +378,7 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
       }
     }
   }
+  __builtin_amdgcn_s_setprio(0);
 }
 
 // SHARE: the workgroup's waves split a tile's rows (16 NT columns), else its columns
