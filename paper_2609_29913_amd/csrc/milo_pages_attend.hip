@@ -13,6 +13,7 @@ namespace {
 constexpr int kPagesThreads = 256;   // four waves
 constexpr int kPagesWaves = kPagesThreads / 64;
 constexpr int kLeastShare = 4;       // positions (64 rows each) of a share, as a rule
+constexpr int kLongShare = 24;       // and before every CU gets a second one
 
 struct PagesArgs {
   milo_pages p;
@@ -425,10 +426,14 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
   }
   X = uniform(X);
   if (a.whole_tiles && (int)blockIdx.x >= X) return;
-  // As many shares as keep kLeastShare each, up to the grid; one for a tile where that is
-  // about as many, so that tiles of like length are not cut.
+  // As many shares as keep kLeastShare each, up to one a CU, or two of kLongShare (8 requests
+  // of 9000 rows, 14B heads: 37.5 us in 256 shares of 37 positions, 42.9 in 512 of 18; 32
+  // requests of 8320 on average, 7B heads, 71.7 in 256, 65.1 in 512 of 33), not in between,
+  // where some CUs have twice the others' work; one for a tile where that is about as many, so
+  // that tiles of like length are not cut.
   int W = X / kLeastShare;
   if (W < 2 * a.least_tiles) W = a.least_tiles;
+  else if (W > (int)gridDim.x / 2) W = X < kLongShare * (int)gridDim.x ? gridDim.x / 2 : gridDim.x;
   W = min(min((int)gridDim.x, W), X / kTileCost);
   if (W >= kXcds) W -= W % kXcds;
   W = max(W, 1);
@@ -883,11 +888,12 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   // Whole tiles, without parts to join, where no request can be long: up to 1024 rows
   // (measured, one request, 7B heads: 1024 rows 10.3 us against 13.3 in shares, 2048 rows
   // 15.7 against 13.4), up to 4096 of many tiles (64 requests, 7B heads, 4096 rows each: 55.9
-  // against 61.9; 0.5B heads 22.3 against 22.0); where many columns make enough tiles, whose
-  // parts would be large (2048 queries after 6144 rows: 276 against 300); and where
-  // positions might not fit 31 bits.
+  // against 61.9; 0.5B heads 22.3 against 22.0); where many columns make tiles enough to even
+  // out (with about as many as workgroups run at once, 2048 queries after 6144 rows take 258 us
+  // whole and 263 in shares, 0.5B heads 177 and 165, 1024 14B queries after 3072 rows 123 and
+  // 114); and where positions might not fit 31 bits.
   const int64_t rows = (int64_t)table_width * pages->page_tokens;
-  a.whole_tiles = rows <= 1024 || (rows <= 4096 && least >= kGrid / 4) || (tiling != kFew && least >= kGrid / 2) ||
+  a.whole_tiles = rows <= 1024 || (rows <= 4096 && least >= kGrid / 4) || (tiling != kFew && least >= 2 * kGrid) ||
                   most * (kTileCost + rows / kRowAlign + 1) > INT32_MAX / 2;
   const int grid = a.whole_tiles ? (int)most : kGrid;
   if (d == 64) launch_pages<64>(a, tiling, grid, s);
