@@ -336,8 +336,9 @@ int milo_block_svd_flops(double* flops);
  *   milo_pages_load    rows back to bf16 (e.g. as the input of milo_block_svd)
  * All four are asynchronous, allocate nothing, copy nothing from or to the host
  * and may be captured into a graph; what they need besides their arguments is
- * in buffers of the caller.  All buffers are device memory of the current
- * device.  Values that only the device knows (lengths, ids, slots) are checked
+ * in buffers of the caller (milo_attend_pages with a cache: as milo_attend_decode
+ * in all of this, so a shape is called once before its capture).  All buffers are
+ * device memory of the current device.  Values that only the device knows (lengths, ids, slots) are checked
  * there: a value out of range never leads to an access out of range; what it
  * does instead is said at each function.
  * ------------------------------------------------------------------------- */
@@ -447,12 +448,14 @@ int milo_pages_load(const milo_pages* pages, const int32_t* slots, int32_t n_tok
  *                milo_attend_decode.  Its workspace is used: order the calls on it.
  *   page_table   [n_req][table_width], lens [n_req]: request i's rows are the first
  *                lens[i] of its pages (lengths are cut to [0, table_width * page_tokens];
- *                a request one of whose pages is outside [0, n_pages) gets NaN)
+ *                a query that sees a row of a page outside [0, n_pages) gets NaN)
  *   q_starts     [n_req + 1] running sums: request i's queries are rows q_starts[i] ..
  *                q_starts[i+1] - 1 of q (cut to [0, n_tok]); NULL: query i is request
- *                i's only one (n_tok == n_req)
+ *                i's only one (n_tok == n_req).  (Of starts that descend somewhere, which
+ *                rows are written, and with what, is undefined.)
  *   q            bf16, row j at q + j * q_stride ([H_q][d]; stride in elements, a multiple
- *                of 8; 16-byte aligned); n_tok >= 0 rows
+ *                of 8; 16-byte aligned; with a cache H_q * d); n_tok >= 0 rows, n_tok * H_q
+ *                at most 2^23
  *   n_q_heads    H_q, a multiple of H_kv, at most 16 query heads per KV head
  *   causal       1: a request's queries are its last rows: query j of m sees the first
  *                lens - m + j + 1 rows.  0: every query sees all rows (cross attention)
@@ -466,7 +469,8 @@ int milo_pages_load(const milo_pages* pages, const int32_t* slots, int32_t n_tok
  * weights enter the value product in fp16 (2^-11) for bf16 output, in two fp16 parts
  * (2^-22) for fp32 output, or to 2^-32 of the row that adds most.  Values of a page and
  * head whose scale is below 2^-96 count as zeros.
- * Errors: INVALID_ARG, UNSUPPORTED, and with a cache those of milo_attend_decode. */
+ * Errors: INVALID_ARG, UNSUPPORTED (also n_req over 2^24), HIP_ERROR, and with a cache
+ * those of milo_attend_decode. */
 #define MILO_OUT_F32 0
 #define MILO_OUT_BF16 1
 int64_t milo_attend_pages_work(int32_t n_req, int32_t n_tok, int32_t n_q_heads, int32_t n_kv_heads,

@@ -25,6 +25,8 @@ __host__ __device__ inline int value_byte(int t, int c, int d) {
   return ((t >> 4) * (d >> 6) + (c >> 6)) * 1024 + ((t & 15) >> 2) * 256 + (c & 15) * 16 + ((c & 63) >> 4) * 4 + (t & 3);
 }
 
+constexpr int kMaxPagesReq = 1 << 24;  // requests of a call
+
 // log2 of the page size, or -1 where it is none of 16, 32, 64, 128
 inline int log2_page(int page_tokens) {
   for (int k = 4; k <= 7; ++k)
@@ -183,6 +185,20 @@ __host__ __device__ inline void next_tile(const Get& get, Place& at, int H, int 
 }
 
 #ifdef __HIPCC__
+
+__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+// sums over the lanes up to this one, which stop at 2^32 - 1
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+#define MILO_FROM(ctrl, rows) x = sat_add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xF, false))
+  MILO_FROM(0x111, 0xF);  // 1, 2, 4, 8 lanes before, in rows of 16
+  MILO_FROM(0x112, 0xF);
+  MILO_FROM(0x114, 0xF);
+  MILO_FROM(0x118, 0xF);
+  MILO_FROM(0x142, 0xA);  // rows 0 and 2 to rows 1 and 3
+  MILO_FROM(0x143, 0xC);  // row 1 to rows 2 and 3
+#undef MILO_FROM
+  return x;
+}
 
 __device__ __forceinline__ float bf16_value(uint32_t bits) { return __uint_as_float(bits << 16); }
 __device__ __forceinline__ uint32_t bf16_bits(float x) {  // round half to even

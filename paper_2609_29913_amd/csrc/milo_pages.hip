@@ -19,7 +19,6 @@ namespace {
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
 constexpr int kFillThreads = 256;
-constexpr int kMaxPlanReq = 1 << 24;
 constexpr int kOneLaunch = 4096;  // new rows that one workgroup writes the slots of
 
 enum PlanStatus : int { kPoolShort = 1, kRowNarrow = 2, kBadLength = 4, kSlotsShort = 8, kBadRing = 16 };
@@ -46,21 +45,8 @@ struct Sums {
   uint32_t rows, taken, given;
 };
 
-__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 __device__ __forceinline__ Sums add(Sums a, Sums b) {
   return {sat_add(a.rows, b.rows), sat_add(a.taken, b.taken), sat_add(a.given, b.given)};
-}
-// sums over the lanes up to this one
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
-#define MILO_FROM(ctrl, rows) x = sat_add(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xF, false))
-  MILO_FROM(0x111, 0xF);  // 1, 2, 4, 8 lanes before, in rows of 16
-  MILO_FROM(0x112, 0xF);
-  MILO_FROM(0x114, 0xF);
-  MILO_FROM(0x118, 0xF);
-  MILO_FROM(0x142, 0xA);  // rows 0 and 2 to rows 1 and 3
-  MILO_FROM(0x143, 0xC);  // row 1 to rows 2 and 3
-#undef MILO_FROM
-  return x;
 }
 
 // what a request of n rows and change delta adds to the sums; *flags: what is wrong with it
@@ -539,7 +525,7 @@ int milo_pages_plan(const int32_t* lens, const int32_t* delta, int32_t n_req, in
                     int32_t* status, void* work, void* hip_stream) {
   clear_error();
   if (n_req < 0 || n_slots < 0) return pages_fail(MILO_ERR_INVALID_ARG, "n_req and n_slots must be >= 0");
-  if (n_req > kMaxPlanReq) return pages_fail(MILO_ERR_UNSUPPORTED, "more than %d requests", kMaxPlanReq);
+  if (n_req > kMaxPagesReq) return pages_fail(MILO_ERR_UNSUPPORTED, "more than %d requests", kMaxPagesReq);
   const int lg = log2_page(page_tokens);
   if (lg < 0) return pages_fail(MILO_ERR_UNSUPPORTED, "page_tokens %d not supported (16, 32, 64 or 128)", page_tokens);
   if (table_width < 1 || n_pages < 1) return pages_fail(MILO_ERR_INVALID_ARG, "table_width and n_pages must be >= 1");

@@ -1,4 +1,19 @@
-// Attention over the paged 8-bit cache (include/milo.h: milo_attend_pages).
+// Attention over the paged 8-bit cache (include/milo.h: milo_attend_pages):
+//   out = sum_r 2^(x_r) v_r / sum_r 2^(x_r),  x_r = scale log2(e) s_page (q . code_r)
+// in one pass over the rows, with the exponent m that the sums are relative to
+// (Running).  The codes go from memory straight into registers in the order the
+// matrix instructions take them, are converted there and used by all columns (query
+// x head of one KV head) of a tile; the scores' registers are, as they stand, the
+// weights' operand of the value product, so nothing goes through LDS but the sums of
+// waves that share a tile.
+// Bounds: few columns a tile read the cache once (14B heads, 64 requests of 8192 rows,
+// E4M3: 1.07 GB in 184 us, 5.8 TB/s, where a copy reaches 5.1; 7B heads, 32 requests of
+// 257 .. 16384 rows, INT8: 0.28 GB in 65 us, 4.3 TB/s, of which 9 us are the start and
+// the join).  Many columns are bound by the vector units' conversions and exponentials,
+// of which each wave does its own (2048 queries after 6144 rows, 7B heads: 255 us, 825
+// TFLOP/s, where a matrix product of 16384^3 reaches 1328).  One request of 131001
+// rows (0.13 GB) takes 39 us, 26 at a copy's rate: the rest is the start of a wave's
+// stream and the join of 256 parts.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -38,7 +53,6 @@ struct PagesArgs {
 __device__ inline int start_of(const PagesArgs& a, int i) {
   return a.starts ? min(max(a.starts[i], 0), a.n_tok) : i;
 }
-
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -97,16 +111,6 @@ __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) {
 }
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-// sums of x over the lanes up to this one
-__device__ __forceinline__ int wave_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // from 1, 2, 4, 8 lanes before, in rows of 16
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // rows 0 and 2 to rows 1 and 3
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // row 1 to rows 2 and 3
-  return x;
-}
 __device__ __forceinline__ int lane_of(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
 __device__ __forceinline__ float lane_of(float v, int l) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l));
@@ -389,7 +393,7 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
   constexpr int GS = NT == 1 ? 4 : 2, ROWS = 16 * GS;
   constexpr int COLS = SHARE ? 16 * NT : 16 * NT * kPagesWaves;
   constexpr int OS = D + 4;  // row stride of a column's partial in LDS
-  __shared__ int wave_cost[kPagesWaves];
+  __shared__ uint32_t wave_cost[kPagesWaves];
   __shared__ Place begin;
   __shared__ Request reqs[kPagesThreads];  // all of them where there are no more than threads
   // two sets in turn: a wave writes a tile's while others still read the last one's
@@ -406,25 +410,27 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
     const Request q = chunk == 1 ? reqs[r] : request_of(a, r);
     return Request{q.start, q.m, q.n};
   };
-  int own = 0;  // of this thread's requests
+  // (sums that stop at 2^32 - 1: only q_starts that are no running sums get there)
+  uint32_t own = 0;  // of this thread's requests
   for (int r = tid * chunk; r < min((tid + 1) * chunk, a.n_req); ++r) {
     const Request q = request_of(a, r);
     if (chunk == 1) reqs[tid] = q;
     const int all = tiles_of(q.m, tt, a.tt_inv);
-    own += a.whole_tiles ? all : tiles_cost(q, all, all, tt, a.causal);
+    own = sat_add(own, a.whole_tiles ? all : tiles_cost(q, all, all, tt, a.causal));
   }
-  own *= H;
-  int upto = wave_scan(own);
+  if ((uint64_t)own * H >> 32) own = ~0u;
+  else own *= H;
+  uint32_t upto = wave_scan(own);
   if (lane == 63) wave_cost[wave] = upto;
   __syncthreads();
-  int X = 0;
+  uint32_t sum = 0;
 #pragma unroll
   for (int k = 0; k < kPagesWaves; ++k) {
-    const int c = wave_cost[k];
-    if (k < wave) upto += c;
-    X += c;
+    const uint32_t c = wave_cost[k];
+    if (k < wave) upto = sat_add(upto, c);
+    sum = sat_add(sum, c);
   }
-  X = uniform(X);
+  const int X = uniform(sum > INT32_MAX / 2 ? 0 : (int)sum);
   if (a.whole_tiles && (int)blockIdx.x >= X) return;
   // As many shares as keep kLeastShare each, up to one a CU, or two of kLongShare (8 requests
   // of 9000 rows, 14B heads: 37.5 us in 256 shares of 37 positions, 42.9 in 512 of 18; 32
@@ -450,12 +456,12 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
   }
 
   // The thread one of whose requests holds position b0 finds the tile.
-  if (b0 < upto && b0 >= upto - own) {
+  if ((uint32_t)b0 < upto && (uint32_t)b0 >= upto - own) {
     Place at;
     if (!a.whole_tiles) {
-      at = place_of(get, tid * chunk, upto - own, b0, H, tt, a.tt_inv, a.causal);
+      at = place_of(get, tid * chunk, (int)(upto - own), b0, H, tt, a.tt_inv, a.causal);
     } else {  // a request's last tiles, which see most, first; its heads side by side
-      int x = b0 - (upto - own);
+      int x = b0 - (int)(upto - own);
       for (at.r = tid * chunk;; ++at.r) {
         at.rq = get(at.r);
         at.all = tiles_of(at.rq.m, tt, a.tt_inv);
@@ -740,6 +746,7 @@ __global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) 
 int64_t round256(int64_t x) { return (x + 255) / 256 * 256; }
 
 constexpr int kGrid = 512;  // workgroups that share the work: two on every CU
+constexpr int64_t kMaxColumns = 1 << 23;  // 256 threads for each of 17 / 16 as many tiles fit a launch's 2^32
 
 // How a call's columns are tiled: 16 or 32 to a workgroup whose waves split the rows where
 // requests bring few queries each, else 128 whose waves split the columns.
@@ -807,6 +814,7 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   if (const int e = check_pages(pages); e != MILO_OK) return e;
   const int H = pages->n_kv_heads, d = pages->head_dim;
   if (n_req < 0 || n_tok < 0) return pages_fail(MILO_ERR_INVALID_ARG, "n_req and n_tok must be >= 0");
+  if (n_req > kMaxPagesReq) return pages_fail(MILO_ERR_UNSUPPORTED, "n_req must be at most 2^24");
   if (!q_starts && n_tok != n_req)
     return pages_fail(MILO_ERR_INVALID_ARG, "without q_starts n_tok (%d) must equal n_req (%d)", n_tok, n_req);
   if (n_q_heads < 1 || n_q_heads % H != 0)
@@ -816,7 +824,8 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   if (table_width < 1) return pages_fail(MILO_ERR_INVALID_ARG, "table_width must be >= 1");
   if ((int64_t)table_width * pages->page_tokens > INT32_MAX)
     return pages_fail(MILO_ERR_UNSUPPORTED, "table_width times page_tokens must be below 2^31");
-  if ((int64_t)n_tok * n_q_heads > (int64_t)1 << 24) return pages_fail(MILO_ERR_UNSUPPORTED, "too many query columns");
+  if ((int64_t)n_tok * n_q_heads > kMaxColumns)
+    return pages_fail(MILO_ERR_UNSUPPORTED, "n_tok times n_q_heads must be at most 2^23");
   if (causal != 0 && causal != 1) return pages_fail(MILO_ERR_INVALID_ARG, "causal must be 0 or 1 (got %d)", causal);
   if (!std::isfinite(scale)) return pages_fail(MILO_ERR_INVALID_ARG, "scale must be finite");
   if (out_format != MILO_OUT_F32 && out_format != MILO_OUT_BF16)
@@ -878,7 +887,7 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   a.lg_page = log2_page(pages->page_tokens);
   a.causal = causal;
   a.out_bf16 = out_format == MILO_OUT_BF16;
-  // tiles at least (each request that has queries has one) and at most
+  // about as many tiles as there are at least (one a request, if each has queries), and at most
   const int tt = tile_columns(tiling) / G;
   const int64_t least = (int64_t)H * std::max((n_tok + tt - 1) / tt, std::min(n_req, n_tok));
   const int64_t most = (int64_t)H * (n_tok / tt + std::min(n_req, n_tok));
@@ -890,8 +899,8 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   // 15.7 against 13.4), up to 4096 of many tiles (64 requests, 7B heads, 4096 rows each: 55.9
   // against 61.9; 0.5B heads 22.3 against 22.0); where many columns make tiles enough to even
   // out (with about as many as workgroups run at once, 2048 queries after 6144 rows take 258 us
-  // whole and 263 in shares, 0.5B heads 177 and 165, 1024 14B queries after 3072 rows 123 and
-  // 114); and where positions might not fit 31 bits.
+  // whole and 263 in shares, 0.5B heads 177 and 165, 1024 14B queries, the last of 4096 rows, 123
+  // and 114); and where positions might not fit 31 bits.
   const int64_t rows = (int64_t)table_width * pages->page_tokens;
   a.whole_tiles = rows <= 1024 || (rows <= 4096 && least >= kGrid / 4) || (tiling != kFew && least >= 2 * kGrid) ||
                   most * (kTileCost + rows / kRowAlign + 1) > INT32_MAX / 2;

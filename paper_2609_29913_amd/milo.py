@@ -652,7 +652,7 @@ def milo_attend_pages(pages: MiloPages, page_table, lens, q, scale: float, out, 
         raise ValueError(f"work holds {work.numel()} bytes, {need} are needed")
     _check(L.milo_attend_pages(
         cache, _i32(table) if n_sel else None, n_sel, p._as_parameter_, page_table.data_ptr(), page_table.shape[1],
-        lens.data_ptr(), _addr(q_starts), n_req, q.data_ptr(), q_stride, n_tok, h_q, 1 if causal else 0, scale,
+        lens.data_ptr(), _addr(q_starts), n_req, q.data_ptr(), q_stride, n_tok, h_q, 1 if causal else 0, float(scale),
         out.data_ptr(), MILO_OUT_F32 if out.dtype is torch.float32 else MILO_OUT_BF16, work.data_ptr(),
         _stream_on(stream, dev)))
 
