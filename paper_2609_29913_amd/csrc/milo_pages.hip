@@ -489,7 +489,10 @@ __global__ __launch_bounds__(kRowThreads) void load_kernel(LoadArgs a) {
     uint4 r = make_uint4(bf16_pair(s[i] * x.x, s[i] * x.y), bf16_pair(s[i] * x.z, s[i] * x.w),
                          bf16_pair(s[i] * y.x, s[i] * y.y), bf16_pair(s[i] * y.z, s[i] * y.w));
     if (!in[i]) r = make_uint4(0, 0, 0, 0);
-    *reinterpret_cast<uint4*>(out + (j0 + i) * stride + h * D + 8 * ch) = r;
+    // past the caches, which the codes then have: 64k rows of 14B heads 85 us against 91, with the
+    // read of them that follows 144 either way; 32k rows 31 against 43
+    typedef uint32_t Line __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(Line, r), reinterpret_cast<Line*>(out + (j0 + i) * stride + h * D + 8 * ch));
   }
 }
 
