@@ -18,6 +18,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "milo_attend.h"
 #include "milo_pages.h"
@@ -676,12 +677,17 @@ struct Joined {
   }
 };
 
+constexpr int kJoinBlocks = 16;  // workgroups for a tile's columns
+
 // Joins the parts of the tile that begins in share w and ends in share we: its own
-// slot and the first slot of the shares after it.  Of few parts, a workgroup's PL lanes
-// of D / 4 threads take a column each; of many, they share CB columns at a time, each
-// every PL-th part in turn, U at once, and are joined in order.
-template <int D, int COLS, int CB>
+// slot and the first slot of the shares after it.  Of few parts, each lane of D / 4
+// threads takes a column; of many, a workgroup's PL lanes share CB columns at a time, each
+// every PL-th part in turn, U at once, and are joined in order.  Bound by the reading of
+// the parts where tiles are wide (456 tiles of 128 columns in two parts each, 60 MB: 18
+// us), else by its start and the chain of a lane's parts (4 tiles of 256 parts: 6 us).
+template <int D, int COLS>
 __global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) {
+  constexpr int CB = COLS / kJoinBlocks < 4 ? COLS / kJoinBlocks : 4;
   constexpr int TPC = D / 4, PL = kPagesThreads / TPC, U = 4;
   static_assert(CB <= PL, "a lane finishes a column");
   __shared__ float2 lane_ml[PL][CB];
@@ -690,25 +696,28 @@ __global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) 
   if (mt.x < 0) return;
   const int s0 = mt.z, we = mt.w, w = s0 >> 1, dq = threadIdx.x % TPC, pl = threadIdx.x / TPC;
   const auto part_at = [&](int k, int c) { return (int64_t)(k == w ? s0 : 2 * k) * COLS + c; };
-  if (we - w < 2 * U) {
-    for (int c = blockIdx.y * PL + pl; c < mt.y; c += gridDim.y * PL) {
-      float2 ml[2 * U];
-      float4 y[2 * U];
+  const auto few = [&](auto n) {  // at most n parts
+    constexpr int N = decltype(n)::value;
+    const int c = blockIdx.y * PL + pl;
+    if (c >= mt.y) return;
+    float2 ml[N];
+    float4 y[N];
 #pragma unroll
-      for (int u = 0; u < 2 * U; ++u) {
-        const int64_t at = part_at(min(w + u, we), c);
-        ml[u] = a.part_ml[at];
-        y[u] = *reinterpret_cast<const float4*>(a.part_o + at * D + 4 * dq);
-      }
-      Joined s;
-#pragma unroll
-      for (int u = 0; u < 2 * U; ++u)
-        if (w + u <= we) s.add(ml[u], y[u]);
-      finish(a, mt.x + col_offset(a, c), 4 * dq, D, s.m, s.l, s.o);
+    for (int u = 0; u < N; ++u) {
+      const int64_t at = part_at(min(w + u, we), c);
+      ml[u] = a.part_ml[at];
+      y[u] = *reinterpret_cast<const float4*>(a.part_o + at * D + 4 * dq);
     }
-    return;
-  }
-  for (int c0 = blockIdx.y * CB; c0 < mt.y; c0 += gridDim.y * CB) {
+    Joined s;
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      if (w + u <= we) s.add(ml[u], y[u]);
+    finish(a, mt.x + col_offset(a, c), 4 * dq, D, s.m, s.l, s.o);
+  };
+  static_assert(PL * kJoinBlocks >= COLS, "a lane for each column");
+  if (we - w == 1) return few(std::integral_constant<int, 2>());
+  if (we - w < 8) return few(std::integral_constant<int, 8>());
+  for (int c0 = blockIdx.y * CB; c0 < mt.y; c0 += kJoinBlocks * CB) {
     Joined s[CB];
     for (int k0 = w + pl; k0 <= we; k0 += PL * U) {
       float2 ml[CB][U];
@@ -764,16 +773,6 @@ void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
   else hipLaunchKernelGGL((pages_kernel<D, FMT, PARTS, 2, false>), dim3(grid), dim3(kPagesThreads), 0, s, a);
 }
 
-template <int D, int COLS>
-void launch_join(const PagesArgs& a, hipStream_t s) {
-  // Where tiles are few, each is in many parts: a workgroup for each column.  Most
-  // workgroups of the grid find no tile and leave.
-  if (a.least_tiles < kGrid / 8)
-    hipLaunchKernelGGL((pages_join_kernel<D, COLS, 1>), dim3(kGrid, 16), dim3(kPagesThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL((pages_join_kernel<D, COLS, 4>), dim3(kGrid, COLS / 32 + 1), dim3(kPagesThreads), 0, s, a);
-}
-
 template <int D>
 void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
   const bool e4m3 = a.p.format == MILO_KV_E4M3;
@@ -785,9 +784,11 @@ void launch_pages(const PagesArgs& a, Tiling t, int grid, hipStream_t s) {
     else launch_pages<D, MILO_KV_INT8, 2>(a, t, grid, s);
   }
   if (a.whole_tiles) return;
-  if (t == kFew) launch_join<D, 16>(a, s);
-  else if (t == kSome) launch_join<D, 32>(a, s);
-  else launch_join<D, 128>(a, s);
+  // most workgroups find no tile and leave
+  const dim3 grid_of_parts(kGrid, kJoinBlocks);
+  if (t == kFew) hipLaunchKernelGGL((pages_join_kernel<D, 16>), grid_of_parts, dim3(kPagesThreads), 0, s, a);
+  else if (t == kSome) hipLaunchKernelGGL((pages_join_kernel<D, 32>), grid_of_parts, dim3(kPagesThreads), 0, s, a);
+  else hipLaunchKernelGGL((pages_join_kernel<D, 128>), grid_of_parts, dim3(kPagesThreads), 0, s, a);
 }
 
 }  // namespace
