@@ -550,7 +550,9 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
           row += ROWS;
           break;
         }
-        if (row + 2 * ROWS < wb) load_step(a, req, g, win, row + 2 * ROWS, last_page, s0);
+        // (the same rows again behind the last: a load that may not be there makes the compiler
+        // wait for the newest one in its stead)
+        load_step(a, req, g, win, row + 2 * ROWS < wb ? row + 2 * ROWS : row + ROWS, last_page, s0);
         add_step<false, D, FMT, PARTS, NT, GS>(s1, qf, row + ROWS, n, vis, run);
       }
       for (; row < wb; row += ROWS) {  // the last ones, whose rows not every column sees
