@@ -6,14 +6,20 @@
 // x head of one KV head) of a tile; the scores' registers are, as they stand, the
 // weights' operand of the value product, so nothing goes through LDS but the sums of
 // waves that share a tile.
-// Bounds: few columns a tile read the cache once (14B heads, 64 requests of 8192 rows,
-// E4M3: 1.07 GB in 184 us, 5.8 TB/s, where a copy reaches 5.1; 7B heads, 32 requests of
-// 257 .. 16384 rows, INT8: 0.28 GB in 65 us, 4.3 TB/s, of which 9 us are the start and
-// the join).  Many columns are bound by the vector units' conversions and exponentials,
-// of which each wave does its own (2048 queries after 6144 rows, 7B heads: 255 us, 825
-// TFLOP/s, where a matrix product of 16384^3 reaches 1328).  One request of 131001
-// rows (0.13 GB) takes 39 us, 26 at a copy's rate: the rest is the start of a wave's
-// stream and the join of 256 parts.
+// Bounds, with measured times between calls:
+//  - few columns a tile: the cache is read once.  14B heads, 64 requests of 8192 rows,
+//    E4M3: 1.08 GB in 182 us, 5.9 TB/s, where a copy moves 5.1 (half of it writes); 7B
+//    heads, 32 requests of 257 .. 16384 rows, INT8: 0.28 GB in 63 us, 4.4 TB/s, of which
+//    5 are the join and about 5 the start.  One request of 131001 rows: 0.13 GB in 39
+//    us, 28 of them reading (4.8 TB/s), 6 the join of 64 parts a tile.
+//  - many columns: the vector units and the matrix units together, which hardly
+//    overlap here (2048 queries, the last of 8192 rows, 7B heads, E4M3: 242 us, 870
+//    TFLOP/s, where a matrix product of 16384^3 reaches 1328; the matrix units are busy
+//    37% of the cycles, the vector units issue in 63% of them).  Half of the vector
+//    instructions are the codes' conversions, which INT8 needs more of (about 310 us).
+//  - in between (32 columns): the latency of a wave's stream of loads (8 requests of
+//    100 .. 3000 rows, 1 .. 37 queries that see all of them, 14B heads: 28 us).
+//  - one short request: the launch (9 us between calls, 7 on the GPU).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -387,8 +393,12 @@ __device__ __forceinline__ void add_step(const Step<D, GS>& st, const bf16x8 (&q
   __builtin_amdgcn_s_setprio(0);
 }
 
-// SHARE: the workgroup's waves split a tile's rows (16 NT columns), else its columns
-// (64 NT columns, every wave reads all rows).
+// One workgroup's share of the call: the tiles, or parts of tiles, between two positions
+// (milo_pages.h).  SHARE: its waves split a tile's rows (16 NT columns) and join their
+// sums through LDS, else its columns (64 NT columns, every wave reads all rows, three of
+// four times from L1).  Two waves to a SIMD, 256 registers each: with one of 64 columns
+// the 2048-query chunk takes 367 us against 266 at the time, since nothing then fills a
+// wave's waits.  Rows are read a step ahead, 64 of them at 16 columns, else 32.
 template <int D, int FMT, int PARTS, int NT, bool SHARE>
 __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
   constexpr int GS = NT == 1 ? 4 : 2, ROWS = 16 * GS;
@@ -686,7 +696,7 @@ constexpr int kJoinBlocks = 16;  // workgroups for a tile's columns
 // threads takes a column; of many, a workgroup's PL lanes share CB columns at a time, each
 // every PL-th part in turn, U at once, and are joined in order.  Bound by the reading of
 // the parts where tiles are wide (456 tiles of 128 columns in two parts each, 60 MB: 18
-// us), else by its start and the chain of a lane's parts (4 tiles of 256 parts: 6 us).
+// us), else by its start and the chain of a lane's parts (4 tiles of 64 parts: 6 us).
 template <int D, int COLS>
 __global__ __launch_bounds__(kPagesThreads) void pages_join_kernel(PagesArgs a) {
   constexpr int CB = COLS / kJoinBlocks < 4 ? COLS / kJoinBlocks : 4;
@@ -760,7 +770,12 @@ constexpr int kGrid = 512;  // workgroups that share the work: two on every CU
 constexpr int64_t kMaxColumns = 1 << 23;  // 256 threads for each of 17 / 16 as many tiles fit a launch's 2^32
 
 // How a call's columns are tiled: 16 or 32 to a workgroup whose waves split the rows where
-// requests bring few queries each, else 128 whose waves split the columns.
+// requests bring few queries each, else 128 whose waves split the columns.  By the average
+// request's columns, so that one kernel serves the call: up to 16 the cache's reading
+// bounds, and 16 columns waste least; up to 112 the tiles of 128 would be few and
+// partly empty (8 requests of 1 .. 37 queries, 14B heads: 36 us in tiles of 32 against 57 in
+// tiles of 64 by columns, when these were measured); beyond, tiles of 32 would
+// read the rows four times.
 enum Tiling { kFew, kSome, kMany };
 Tiling tiling_of(int32_t n_req, int32_t n_tok, int G) {
   const int64_t cols = (int64_t)n_tok * G;
