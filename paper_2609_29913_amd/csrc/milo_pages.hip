@@ -221,11 +221,9 @@ __global__ __launch_bounds__(kFillThreads) void plan_fill_kernel(PlanArgs a) {
 // holds two groups.  The new rows of 16 tokens stay in registers between the maximum and
 // the codes, so they are read once; larger runs are read twice, the second time from L2.
 // Measured: store, 4200 rows of 4 KV heads of 128 dims (13 MB in and out) 8.3 us, 64
-// single rows of 8 heads 6.4, of which about 4 are the chain slot, scale,
-// codes, code stores; load, 64k rows of 8 heads (131 MB of codes to 262 MB) 84 us, the 5.2
-// TB/s that a copy reaches with the 40 MB of codes that it reads twice (values' dwords
-// of many waves pass through L1 and partly L2 before a line's last is taken); 1k rows
-// of 4 heads 3.9 us.
+// single rows of 8 heads 6.4 (slot, scale, codes and stores wait for one another); load,
+// 64k rows of 8 heads (131 MB of codes to 262 MB) 84 us, a copy's 5.2 TB/s counting the 40
+// MB of codes that are fetched a second time; 1k rows of 4 heads 3.9 us.
 // ---------------------------------------------------------------------------
 constexpr int kRowThreads = 256;
 
