@@ -483,14 +483,17 @@ def _pages_arg(pages) -> MiloPages:
     return pages
 
 
-def _i32_dev(x, name: str, dev: int, *shape: int):
-    """A contiguous int32 tensor on GPU `dev` of the given shape (-1: any)."""
-    if not isinstance(x, torch.Tensor) or x.dtype is not torch.int32 or x.get_device() != dev or not x.is_contiguous():
-        _dev_tensor(x, name, ("torch.int32",))
-    got = x.shape
-    if len(got) != len(shape) or (shape[0] != got[0] and shape[0] >= 0):
-        raise ValueError(f"{name} has shape {tuple(got)}, expected {tuple(shape)}")
-    return x
+def _i32_dev(x, name: str, dev: int, shape):
+    """A contiguous int32 tensor on GPU `dev` of the given shape, or number of dimensions."""
+    try:
+        if x.dtype is torch.int32 and x.get_device() == dev and x.is_contiguous() and \
+                (x.shape == shape or x.dim() == shape):
+            return x
+    except AttributeError:
+        pass
+    _dev_tensor(x, name, ("torch.int32",))
+    raise ValueError(f"{name} has shape {tuple(x.shape)}, expected " +
+                     (f"{shape} dimension(s)" if isinstance(shape, int) else f"{shape}"))
 
 
 def _row_stride(x, name: str, dev: int, heads: int, d: int) -> int:
@@ -543,22 +546,24 @@ def milo_pages_plan(lens, delta, page_tokens: int, table, ring, ring_state, n_sl
     if not isinstance(lens, torch.Tensor) or not lens.is_cuda or lens.dim() != 1:
         raise ValueError("lens must be an int32 GPU tensor [n_req]")
     n_req, dev = lens.shape[0], torch.cuda.current_device()
-    _i32_dev(lens, "lens", dev, n_req)
-    _i32_dev(delta, "delta", dev, n_req)
-    _i32_dev(table, "table", dev, n_req, -1)
-    _i32_dev(ring, "ring", dev, -1)
-    _i32_dev(ring_state, "ring_state", dev, 2)
+    per_req = (n_req,)
+    _i32_dev(lens, "lens", dev, per_req)
+    _i32_dev(delta, "delta", dev, per_req)
+    if _i32_dev(table, "table", dev, 2).shape[0] != n_req:
+        raise ValueError(f"table has {table.shape[0]} rows for {n_req} requests")
+    _i32_dev(ring, "ring", dev, 1)
+    _i32_dev(ring_state, "ring_state", dev, (2,))
     if slots is not None:
-        _i32_dev(slots, "slots", dev, -1 if n_slots is None else n_slots)
+        _i32_dev(slots, "slots", dev, 1 if n_slots is None else (n_slots,))
     elif n_slots is None:
         raise ValueError("give slots, or n_slots for a new one")
     need = lib().milo_pages_plan_work(n_req)
-    if work is not None and _i32_dev(work, "work", dev, -1).numel() * 4 < need:
+    if work is not None and _i32_dev(work, "work", dev, 1).numel() * 4 < need:
         raise ValueError(f"work holds {work.numel() * 4} bytes, {need} are needed")
-    for name, x, n in (("lens_out", lens_out, n_req), ("ring_state_out", ring_state_out, 2), ("starts", starts, n_req + 1),
-                       ("status", status, 1)):
+    for name, x, shape in (("lens_out", lens_out, per_req), ("ring_state_out", ring_state_out, (2,)),
+                           ("starts", starts, (n_req + 1,)), ("status", status, (1,))):
         if x is not None:
-            _i32_dev(x, name, dev, n)
+            _i32_dev(x, name, dev, shape)
     if lens_out is None or ring_state_out is None or starts is None or slots is None or status is None or work is None:
         with _on_stream(stream):
             def made(x, n):
@@ -580,7 +585,7 @@ def milo_pages_store(pages: MiloPages, k, v, slots, stream=None) -> None:
     n = k.shape[0]
     if v.shape[0] != n:
         raise ValueError(f"k has {n} rows, v {v.shape[0]}")
-    _i32_dev(slots, "slots", dev, n)
+    _i32_dev(slots, "slots", dev, (n,))
     _check(lib().milo_pages_store(p._as_parameter_, k.data_ptr(), ks, v.data_ptr(), vs, slots.data_ptr(), n,
                                   _stream_on(stream, dev)))
 
@@ -589,7 +594,7 @@ def milo_pages_load(pages: MiloPages, slots, k_out=None, v_out=None, stream=None
     """Rows of `slots` (int32 [n]) back to bf16 into k_out and / or v_out [n][H_kv][d]."""
     p = _pages_arg(pages)
     dev, width = p.device.index, p.n_kv_heads * p.head_dim
-    _i32_dev(slots, "slots", dev, -1)
+    _i32_dev(slots, "slots", dev, 1)
     n = slots.shape[0]
     if k_out is None and v_out is None:
         raise ValueError("k_out and v_out are both None")
@@ -626,11 +631,11 @@ def milo_attend_pages(pages: MiloPages, page_table, lens, q, scale: float, out, 
         _dev_tensor(out, "out", ("torch.float32", "torch.bfloat16"))
     if out.shape != q.shape:
         raise ValueError(f"out shape {tuple(out.shape)} differs from q shape {tuple(q.shape)}")
-    _i32_dev(lens, "lens", dev, -1)
-    n_req = lens.shape[0]
-    _i32_dev(page_table, "page_table", dev, n_req, -1)
+    n_req = _i32_dev(lens, "lens", dev, 1).shape[0]
+    if _i32_dev(page_table, "page_table", dev, 2).shape[0] != n_req:
+        raise ValueError(f"page_table has {page_table.shape[0]} rows for {n_req} requests")
     if q_starts is not None:
-        _i32_dev(q_starts, "q_starts", dev, n_req + 1)
+        _i32_dev(q_starts, "q_starts", dev, (n_req + 1,))
     table, n_sel = None, 0
     if block_table is not None:
         table = np.asarray(block_table, dtype=np.int32).reshape(-1)
