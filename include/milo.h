@@ -469,8 +469,9 @@ int milo_pages_load(const milo_pages* pages, const int32_t* slots, int32_t n_tok
  * weights enter the value product in fp16 (2^-11) for bf16 output, in two fp16 parts
  * (2^-22) for fp32 output, or to 2^-32 of the row that adds most.  Values of a page and
  * head whose scale is below 2^-96 count as zeros.
- * Errors: INVALID_ARG, UNSUPPORTED (also n_req over 2^24), HIP_ERROR, and with a cache
- * those of milo_attend_decode. */
+ * Errors: INVALID_ARG, UNSUPPORTED (also n_req over 2^24, and thousands of requests
+ * whose tables allow for about 2^36 rows of all KV heads together), HIP_ERROR, and with
+ * a cache those of milo_attend_decode. */
 #define MILO_OUT_F32 0
 #define MILO_OUT_BF16 1
 int64_t milo_attend_pages_work(int32_t n_req, int32_t n_tok, int32_t n_q_heads, int32_t n_kv_heads,

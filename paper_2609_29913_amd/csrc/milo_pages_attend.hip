@@ -864,6 +864,27 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
   PagesArgs a{};
   const Tiling tiling = tiling_of(n_req, n_tok, G);
+  // about as many tiles as there are at least (one a request, if each has queries), and at most
+  const int tt = tile_columns(tiling) / G;
+  const int64_t least = (int64_t)H * std::max((n_tok + tt - 1) / tt, std::min(n_req, n_tok));
+  const int64_t most = (int64_t)H * (n_tok / tt + std::min(n_req, n_tok));
+  // Whole tiles, without parts to join, where no request can be long: up to 1024 rows
+  // (measured, one request, 7B heads: 1024 rows 10.3 us against 13.3 in shares, 2048 rows
+  // 15.7 against 13.4), up to 4096 of many tiles (64 requests, 7B heads, 4096 rows each: 55.9
+  // against 61.9; 0.5B heads 22.3 against 22.0); and where many columns make tiles enough to
+  // even out (with about as many as workgroups run at once, 2048 queries after 6144 rows take
+  // 258 us whole and 263 in shares, 0.5B heads 177 and 165, 1024 14B queries, the last of 4096
+  // rows, 123 and 114).  Not where there are many requests, since every workgroup reads them
+  // all (requests of up to 64 rows: 1024 of 0.5B heads 27 us whole and 36 in shares, 2048 101
+  // and 62, 512 of 14B heads 59 and 68, 1024 138 and 74).  Where positions might not fit 31
+  // bits (a table far wider than any request), whole tiles or nothing.
+  const int64_t rows = (int64_t)table_width * pages->page_tokens;
+  const bool fit = most * (kTileCost + rows / kRowAlign + 1) <= INT32_MAX / 2;
+  if (!fit && most * n_req > (int64_t)1 << 26)
+    return pages_fail(MILO_ERR_UNSUPPORTED, "%d requests of up to %lld rows are too many for one call", n_req, (long long)rows);
+  a.whole_tiles = !fit || (most * n_req <= (int64_t)1 << 22 &&
+                           (rows <= 1024 || (rows <= 4096 && least >= kGrid / 4) ||
+                            (tiling != kFew && least >= 2 * kGrid)));
   const int64_t slot_cols = 2 * kGrid * tile_columns(tiling);
   char* w = static_cast<char*>(work);
   a.meta = reinterpret_cast<int4*>(w);
@@ -905,23 +926,9 @@ int milo_attend_pages(milo_cache* cache, const int32_t* block_table, int32_t n_s
   a.lg_page = log2_page(pages->page_tokens);
   a.causal = causal;
   a.out_bf16 = out_format == MILO_OUT_BF16;
-  // about as many tiles as there are at least (one a request, if each has queries), and at most
-  const int tt = tile_columns(tiling) / G;
-  const int64_t least = (int64_t)H * std::max((n_tok + tt - 1) / tt, std::min(n_req, n_tok));
-  const int64_t most = (int64_t)H * (n_tok / tt + std::min(n_req, n_tok));
   a.least_tiles = (int)std::min<int64_t>(kGrid, least);
   a.G_inv = (65536 + G - 1) / G;
   a.tt_inv = reciprocal(tt);
-  // Whole tiles, without parts to join, where no request can be long: up to 1024 rows
-  // (measured, one request, 7B heads: 1024 rows 10.3 us against 13.3 in shares, 2048 rows
-  // 15.7 against 13.4), up to 4096 of many tiles (64 requests, 7B heads, 4096 rows each: 55.9
-  // against 61.9; 0.5B heads 22.3 against 22.0); where many columns make tiles enough to even
-  // out (with about as many as workgroups run at once, 2048 queries after 6144 rows take 258 us
-  // whole and 263 in shares, 0.5B heads 177 and 165, 1024 14B queries, the last of 4096 rows, 123
-  // and 114); and where positions might not fit 31 bits.
-  const int64_t rows = (int64_t)table_width * pages->page_tokens;
-  a.whole_tiles = rows <= 1024 || (rows <= 4096 && least >= kGrid / 4) || (tiling != kFew && least >= 2 * kGrid) ||
-                  most * (kTileCost + rows / kRowAlign + 1) > INT32_MAX / 2;
   const int grid = a.whole_tiles ? (int)most : kGrid;
   if (d == 64) launch_pages<64>(a, tiling, grid, s);
   else launch_pages<128>(a, tiling, grid, s);

@@ -31,6 +31,15 @@ def test_attend_hundreds_of_requests(longest, counts):
     assert torch.equal(got, b.run())
 
 
+def test_attend_thousands_of_short_requests():
+    """Too many for every workgroup of a whole tile to read them: shares of many tiles each."""
+    rng = np.random.default_rng(8)
+    b = Batch(8, list(rng.integers(0, 60, 3000)), list(rng.integers(0, 3, 3000)), HEADS["0.5b"], 16, "e4m3")
+    got = b.run()
+    b.check(got, b.want(True))
+    assert torch.equal(got, b.run())
+
+
 @pytest.mark.parametrize("req,counts,heads", [(4, 820, "14b"), (200, 5, "14b")])
 def test_attend_whole_tiles_of_many_columns(req, counts, heads):
     rng = np.random.default_rng(req)

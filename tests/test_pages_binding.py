@@ -71,7 +71,8 @@ def test_load_refuses(args):
     (dict(scale=float("inf")), INV), (dict(out_format=2), INV), (dict(page_table=None), INV), (dict(lens=None), INV),
     (dict(q=None), INV), (dict(q=A + 2), INV), (dict(q_stride=192), INV), (dict(q_stride=260), INV), (dict(out=None), INV),
     (dict(out=A + 8), INV), (dict(work=None), INV), (dict(work=A + 128), INV), (dict(n_sel=1), INV),
-    (dict(n_tok=1 << 23), UNS), (dict(n_tok=(1 << 21) + 1), UNS), (dict(n_req=(1 << 24) + 1), UNS)])
+    (dict(n_tok=1 << 23), UNS), (dict(n_tok=(1 << 21) + 1), UNS), (dict(n_req=(1 << 24) + 1), UNS),
+    (dict(n_req=1 << 14, n_tok=1 << 14, table_width=1 << 22), UNS)])
 def test_attend_refuses(kw, code):
     assert attend(**kw) == code and milo.milo_last_error()
 
