@@ -166,13 +166,14 @@ __device__ inline void finish(const PagesArgs& a, int64_t col, int d, int D, flo
   }
 }
 
-// Pages of one request as a wave reads them: lane i holds the id and scales of page
-// base + i, so a step takes them without waiting for memory.  The values' scale stands
+// Pages of one request as a wave reads them: lane i holds where the head's codes of page
+// base + i begin and its scales, so a step takes them without waiting for memory.  The values' scale stands
 // as its logarithm, which joins the score (see add_step), and as its reciprocal; a
 // page of less than 2^-96 (none at all, as a rule) adds no values: it counts with the least
 // of the other scales, and its reciprocal is negative.
 struct Window {
   int base, id;
+  uint32_t lo, hi;  // first byte of the page and head
   float ks;        // scale of the keys, times the call's, in log2 units
   float lv, rv;    // log2 of the values' scale, 1 / scale
 };
@@ -185,10 +186,13 @@ __device__ inline void window_ids(const PagesArgs& a, int req, int base, int las
   w.id = a.table[(int64_t)req * a.width + min(base + (int)(threadIdx.x & 63), last_page)];
 }
 
+template <int D>
 __device__ inline void window_loads(const PagesArgs& a, int head, Window& w) {
   const bool in = (uint32_t)w.id < (uint32_t)a.p.n_pages;
   if (!in) w.id = 0;
-  const int64_t at = (int64_t)w.id * a.p.n_kv_heads + head;
+  const int64_t at = (int64_t)w.id * a.p.n_kv_heads + head, byte = (at << a.lg_page) * D;
+  w.lo = (uint32_t)byte;
+  w.hi = (uint32_t)(byte >> 32);
   w.ks = a.p.k_scale[at];
   w.lv = a.p.v_scale[at];
   w.rv = in ? 1.f : __uint_as_float(0x7FC00000u);
@@ -223,18 +227,18 @@ struct Step {
 template <int D, int GS>
 __device__ __forceinline__ void load_codes(const PagesArgs& a, int head, const Window& w, int row, int last_page,
                                            Step<D, GS>& st) {
-  const int P = 1 << a.lg_page, lane = threadIdx.x & 63;
-  const int64_t head_bytes = (int64_t)P * D, page_bytes = head_bytes * a.p.n_kv_heads;
+  const uint32_t lane16 = 16 * (threadIdx.x & 63);
 #pragma unroll
   for (int g = 0; g < GS; ++g) {
-    const int r = row + 16 * g, li = min(min(r >> a.lg_page, last_page) - w.base, 63);
-    const int64_t at = lane_of(w.id, li) * page_bytes + head * head_bytes + (r & (P - 1)) * D;
+    const int r = row + 16 * g, li = min(r >> a.lg_page, last_page) - w.base;
+    const int64_t at = ((int64_t)lane_of((int)w.hi, li) << 32 | (uint32_t)lane_of((int)w.lo, li)) +
+                       (r & ((1 << a.lg_page) - 1)) * D;
     const uint8_t* kp = static_cast<const uint8_t*>(a.p.k_codes) + at;
     const uint8_t* vp = static_cast<const uint8_t*>(a.p.v_codes) + at;
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
-      st.k[g][j] = *reinterpret_cast<const uint4*>(kp + 1024 * j + 16 * lane);
-      st.v[g][j] = *reinterpret_cast<const uint4*>(vp + 1024 * j + 16 * lane);
+      st.k[g][j] = *reinterpret_cast<const uint4*>(kp + 1024 * j + lane16);
+      st.v[g][j] = *reinterpret_cast<const uint4*>(vp + 1024 * j + lane16);
     }
   }
 }
@@ -244,7 +248,7 @@ __device__ __forceinline__ void take_scales(const PagesArgs& a, const Window& w,
   st.plain = true;
 #pragma unroll
   for (int g = 0; g < GS; ++g) {
-    const int li = min(min((row + 16 * g) >> a.lg_page, last_page) - w.base, 63);
+    const int li = min((row + 16 * g) >> a.lg_page, last_page) - w.base;
     st.ks[g] = lane_of(w.ks, li);
     st.lv[g] = lane_of(w.lv, li);
     st.rv[g] = lane_of(w.rv, li);
@@ -257,7 +261,7 @@ __device__ __forceinline__ void load_step(const PagesArgs& a, int req, int head,
                                           Step<D, GS>& st) {
   if ((row >> a.lg_page) - w.base >= 64) {
     window_ids(a, req, row >> a.lg_page, last_page, w);
-    window_loads(a, head, w);
+    window_loads<D>(a, head, w);
     window_scales(a, w);
   }
   load_codes(a, head, w, row, last_page, st);
@@ -547,7 +551,7 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
     wb = uniform(wb);
     if (works) {
       Step<D, GS> s0, s1;
-      window_loads(a, g, win);
+      window_loads<D>(a, g, win);
       load_codes(a, g, win, wa, last_page, s0);
       window_scales(a, win);
       take_scales(a, win, wa, last_page, s0);
