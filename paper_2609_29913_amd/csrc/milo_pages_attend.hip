@@ -8,17 +8,17 @@
 // waves that share a tile.
 // Bounds, with measured times between calls:
 //  - few columns a tile: the cache is read once.  14B heads, 64 requests of 8192 rows,
-//    E4M3: 1.08 GB in 182 us, 5.9 TB/s, where a copy moves 5.1 (half of it writes); 7B
-//    heads, 32 requests of 257 .. 16384 rows, INT8: 0.28 GB in 63 us, 4.4 TB/s, of which
-//    5 are the join and about 5 the start.  One request of 131001 rows: 0.13 GB in 39
-//    us, 28 of them reading (4.8 TB/s), 6 the join of 64 parts a tile.
+//    E4M3: 1.08 GB in 182 .. 186 us, 5.8 TB/s, where a copy moves 5.1 (half of it
+//    writes); 7B heads, 32 requests of 257 .. 16384 rows, INT8: 0.28 GB in 63 us, 4.4
+//    TB/s, of which 5 are the join and about 5 the start.  One request of 131001 rows:
+//    0.13 GB in 39 us, 28 of them reading (4.8 TB/s), 6 the join of 64 parts a tile.
 //  - many columns: the vector units and the matrix units together, which hardly
-//    overlap here (2048 queries, the last of 8192 rows, 7B heads, E4M3: 242 us, 870
+//    overlap here (2048 queries, the last of 8192 rows, 7B heads, E4M3: 241 us, 870
 //    TFLOP/s, where a matrix product of 16384^3 reaches 1328; the matrix units are busy
 //    37% of the cycles, the vector units issue in 63% of them).  Half of the vector
 //    instructions are the codes' conversions, which INT8 needs more of (about 310 us).
-//  - in between (32 columns): the latency of a wave's stream of loads (8 requests of
-//    100 .. 3000 rows, 1 .. 37 queries that see all of them, 14B heads: 28 us).
+//  - in between (32 columns): the longest tile (8 requests of 100 .. 3000 rows, 1 .. 37
+//    queries that see all of them, 14B heads: 27 us; the first tiles end after 9).
 //  - one short request: the launch (9 us between calls, 7 on the GPU).
 #include <hip/hip_runtime.h>
 
