@@ -348,7 +348,7 @@ int milo_block_svd_flops(double* flops);
  * row's value is scale * code.  Slot page * page_tokens + offset names one row.
  *   n_pages      >= 1, n_pages * page_tokens <= 2^31 - 1
  *   page_tokens  16, 32, 64 or 128
- *   n_kv_heads   H_kv >= 1
+ *   n_kv_heads   H_kv, 1 to 32767
  *   head_dim     d, 64 or 128
  *   format       MILO_KV_INT8   codes -127 .. 127; scale = amax / 127 (fp32,
  *                               correctly rounded), code = round-half-even(x / scale)
@@ -415,9 +415,9 @@ int milo_pages_plan(const int32_t* lens, const int32_t* delta, int32_t n_req, in
 
 /* Quantise n_tok rows of keys and values into their slots.  Row j's keys are
  * k + j * k_stride (bf16 [H_kv][d], the stride in elements, a multiple of 8;
- * 16-byte aligned), its values likewise.  slots [n_tok]: row j's slot; a slot
- * outside [0, n_pages * page_tokens) skips its row.  Rows of one page must follow
- * one another in the call with ascending slots without gaps, as milo_pages_plan
+ * 16-byte aligned), its values likewise; n_tok at most 2^27.  slots [n_tok]: row j's
+ * slot; a slot outside [0, n_pages * page_tokens) skips its row.  Rows of one page must
+ * follow one another in the call with ascending slots without gaps, as milo_pages_plan
  * gives them, and a page appears once (otherwise the codes and scales of the pages
  * concerned, of no other, are undefined).
  * Rows of a page before its first new one are held: where a new row needs a larger
@@ -433,7 +433,8 @@ int milo_pages_store(const milo_pages* pages, const uint16_t* k, int64_t k_strid
 
 /* Rows of pages as bf16 (scale * code in fp32, rounded once): row j of k_out / v_out
  * ([H_kv][d] each, strides in elements, multiples of 8, 16-byte aligned) is the row in
- * slot slots[j]; zeros for a slot out of range.  Any order, also the same slot twice.
+ * slot slots[j]; zeros for a slot out of range.  Any order, also the same slot twice; n_tok
+ * at most 2^27.
  * k_out or v_out may be NULL (not read then).  Errors: INVALID_ARG, UNSUPPORTED, HIP_ERROR. */
 int milo_pages_load(const milo_pages* pages, const int32_t* slots, int32_t n_tok, uint16_t* k_out,
                     int64_t k_stride, uint16_t* v_out, int64_t v_stride, void* hip_stream);

@@ -25,7 +25,9 @@ __host__ __device__ inline int value_byte(int t, int c, int d) {
   return ((t >> 4) * (d >> 6) + (c >> 6)) * 1024 + ((t & 15) >> 2) * 256 + (c & 15) * 16 + ((c & 63) >> 4) * 4 + (t & 3);
 }
 
-constexpr int kMaxPagesReq = 1 << 24;  // requests of a call
+constexpr int kMaxPagesReq = 1 << 24;   // requests of a call
+constexpr int kMaxPagesRows = 1 << 27;  // rows stored or loaded by a call: a launch has 2^32 threads at most
+constexpr int kMaxPagesHeads = 32767;   // KV heads: a launch has 65536 workgroups at most in y
 
 // log2 of the page size, or -1 where it is none of 16, 32, 64, 128
 inline int log2_page(int page_tokens) {
@@ -53,8 +55,8 @@ inline int check_pages(const milo_pages* p) {
     return pages_fail(MILO_ERR_UNSUPPORTED, "page_tokens %d not supported (16, 32, 64 or 128)", p->page_tokens);
   if (p->head_dim != 64 && p->head_dim != 128)
     return pages_fail(MILO_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", p->head_dim);
-  if (p->n_kv_heads > 65535)
-    return pages_fail(MILO_ERR_UNSUPPORTED, "n_kv_heads %d not supported (at most 65535)", p->n_kv_heads);
+  if (p->n_kv_heads > kMaxPagesHeads)
+    return pages_fail(MILO_ERR_UNSUPPORTED, "n_kv_heads %d not supported (at most %d)", p->n_kv_heads, kMaxPagesHeads);
   if ((int64_t)p->n_pages * p->page_tokens > INT32_MAX)
     return pages_fail(MILO_ERR_UNSUPPORTED, "%d pages of %d tokens exceed 2^31 - 1 slots", p->n_pages, p->page_tokens);
   if (p->format != MILO_KV_INT8 && p->format != MILO_KV_E4M3)

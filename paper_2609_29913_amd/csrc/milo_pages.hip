@@ -586,6 +586,7 @@ int milo_pages_store(const milo_pages* pages, const uint16_t* k, int64_t k_strid
   clear_error();
   if (const int e = check_pages(pages); e != MILO_OK) return e;
   if (n_tok < 0) return pages_fail(MILO_ERR_INVALID_ARG, "n_tok must be >= 0");
+  if (n_tok > kMaxPagesRows) return pages_fail(MILO_ERR_UNSUPPORTED, "n_tok must be at most 2^27");
   if (n_tok == 0) return MILO_OK;
   const int64_t D = (int64_t)pages->n_kv_heads * pages->head_dim;
   if (const int e = check_rows("k", k, k_stride, D); e != MILO_OK) return e;
@@ -618,6 +619,7 @@ int milo_pages_load(const milo_pages* pages, const int32_t* slots, int32_t n_tok
   clear_error();
   if (const int e = check_pages(pages); e != MILO_OK) return e;
   if (n_tok < 0) return pages_fail(MILO_ERR_INVALID_ARG, "n_tok must be >= 0");
+  if (n_tok > kMaxPagesRows) return pages_fail(MILO_ERR_UNSUPPORTED, "n_tok must be at most 2^27");
   if (n_tok == 0) return MILO_OK;
   if (!k_out && !v_out) return pages_fail(MILO_ERR_INVALID_ARG, "k_out and v_out are both NULL");
   const int64_t D = (int64_t)pages->n_kv_heads * pages->head_dim;

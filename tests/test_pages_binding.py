@@ -23,7 +23,7 @@ BAD_POOLS = [(dict(n_pages=0), INV), (dict(n_kv_heads=0), INV), (dict(page_token
              (dict(page_tokens=256), UNS), (dict(head_dim=96), UNS), (dict(format=2), INV), (dict(format=-1), INV),
              (dict(k_codes=None), INV), (dict(v_codes=None), INV), (dict(k_scale=None), INV), (dict(v_scale=None), INV),
              (dict(k_codes=A + 8), INV), (dict(v_codes=A + 4), INV), (dict(n_pages=1 << 27), UNS),
-             (dict(n_kv_heads=1 << 17), UNS)]
+             (dict(n_kv_heads=1 << 17), UNS), (dict(n_kv_heads=32768), UNS)]
 
 
 def attend(p=None, **kw):
@@ -41,6 +41,12 @@ def test_bad_pools(kw, code):
     assert L.milo_pages_store(p, A, 128, A, 128, A, 3, None) == code and milo.milo_last_error()
     assert L.milo_pages_load(p, A, 3, A, 128, A, 128, None) == code
     assert attend(p) == code
+
+
+def test_more_rows_than_a_launch_takes():
+    L, p = milo.lib(), ctypes.byref(pool())
+    assert L.milo_pages_store(p, A, 128, A, 128, A, (1 << 27) + 1, None) == UNS
+    assert L.milo_pages_load(p, A, (1 << 27) + 1, A, 128, A, 128, None) == UNS
 
 
 def test_null_pool():
