@@ -84,11 +84,29 @@ inline int check_rows(const char* name, const void* p, int64_t stride, int64_t w
 // head by KV head, tile by tile, the first k tiles of a head kTileCost k + (vis(0) + ..
 // + vis(k - 1)) / kRowAlign long, rounded down (requests without queries take none).
 // Share w of W has the positions [w L, (w + 1) L) of X, L = ceil(X / W), in whatever tiles
-// they fall, so lengths may differ as they like (the last shares may be short or empty); a
-// tile's rows are cut at multiples of kRowAlign.  All of it follows from the lengths, on the
+// they fall (or a sixth more or less, share_at), so lengths may differ as they like (the
+// last shares may be short or empty); a tile's rows are cut at multiples of kRowAlign.  All of it follows from the lengths, on the
 // device; the host sees to it that X fits 31 bits.
 constexpr int kRowAlign = 64;
 constexpr int kTileCost = 2;  // what a tile costs besides its rows
+
+constexpr int kCus = 256;
+constexpr int kXcdCus = kCus / kXcds;
+
+// Where share k begins.  Of two shares to a CU, the workgroup that came first is served first
+// (with equal shares of a 2048-query chunk it ends after 211 us, the other after 254): the
+// first kXcdCus of an XCD's shares have La positions, the others 2 L - La.  La = L: all alike.
+__host__ __device__ inline int64_t share_at(int k, int L, int La) {
+  if (La == L) return (int64_t)k * L;
+  const int j = k % (2 * kXcdCus);
+  return (int64_t)(k - j) * L + (j < kXcdCus ? j * La : kXcdCus * La + (j - kXcdCus) * (2 * L - La));
+}
+// the share that holds a position
+__host__ __device__ inline int share_of(int pos, int L, int La) {
+  if (La == L) return (int)((uint32_t)pos / (uint32_t)L);
+  const int xcd = pos / (2 * kXcdCus * L), rest = pos - xcd * 2 * kXcdCus * L;
+  return 2 * kXcdCus * xcd + (rest < kXcdCus * La ? rest / La : kXcdCus + (rest - kXcdCus * La) / (2 * L - La));
+}
 
 struct Request {
   int start, m, n;  // first query, queries, rows held

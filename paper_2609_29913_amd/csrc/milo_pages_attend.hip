@@ -13,10 +13,10 @@
 //    TB/s, of which 5 are the join and about 5 the start.  One request of 131001 rows:
 //    0.13 GB in 39 us, 28 of them reading (4.8 TB/s), 6 the join of 64 parts a tile.
 //  - many columns: the vector units and the matrix units together, which hardly
-//    overlap here (2048 queries, the last of 8192 rows, 7B heads, E4M3: 241 us, 870
+//    overlap here (2048 queries, the last of 8192 rows, 7B heads, E4M3: 232 us, 905
 //    TFLOP/s, where a matrix product of 16384^3 reaches 1328; the matrix units are busy
 //    37% of the cycles, the vector units issue in 63% of them).  Half of the vector
-//    instructions are the codes' conversions, which INT8 needs more of (about 310 us).
+//    instructions are the codes' conversions, which INT8 needs more of (about 300 us).
 //  - in between (32 columns): the longest tile (8 requests of 100 .. 3000 rows, 1 .. 37
 //    queries that see all of them, 14B heads: 27 us; the first tiles end after 9).
 //  - one short request: the launch (9 us between calls, 7 on the GPU).
@@ -459,15 +459,20 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
   if (W >= kXcds) W -= W % kXcds;
   W = max(W, 1);
   const int L = uniform((int)((uint32_t)(X + W - 1) / (uint32_t)W));
+  // A sixth more for the first workgroup of a CU and less for the second where tiles are cut
+  // anyway (2048-query chunk 254 -> 243 us, 32 requests of 8320 rows on average, 14B heads,
+  // 122 -> 111; as many uniform tiles as shares, which this would cut: 186 -> 193).
+  const int La = W == 2 * kCus && a.least_tiles < W ? L + L / 6 : L;
   int4* meta = a.meta + blockIdx.x;
   // consecutive shares on one XCD, whose L2 then holds the rows that tiles share
   const int w = W >= kXcds ? (int)(blockIdx.x % kXcds) * (W / kXcds) + blockIdx.x / kXcds : blockIdx.x;
   int b0 = blockIdx.x, b1 = 0;
   if (!a.whole_tiles) {
     if (tid == 0) *meta = make_int4(-1, 0, 0, 0);
-    if ((int)blockIdx.x >= W || w * (int64_t)L >= X) return;
-    b0 = w * L;
-    b1 = min(b0 + L, X);
+    if ((int)blockIdx.x >= W) return;
+    b0 = (int)min((int64_t)X, share_at(w, L, La));
+    b1 = (int)min((int64_t)X, share_at(w + 1, L, La));
+    if (b0 >= b1) return;
   }
 
   // The thread one of whose requests holds position b0 finds the tile.
@@ -667,7 +672,7 @@ __global__ __launch_bounds__(kPagesThreads, 2) void pages_kernel(PagesArgs a) {
     }
     // a tile that begins here and goes on in the next workgroups: joined afterwards
     if (tid == 0 && b0 <= p0 && b1 < p1) {
-      const int we = (p1 - 1) / L;
+      const int we = share_of(p1 - 1, L, La);
       *meta = make_int4((int)q0, ncol, slot, we);
     }
     first = false;

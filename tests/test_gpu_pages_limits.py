@@ -31,6 +31,22 @@ def test_attend_hundreds_of_requests(longest, counts):
     assert torch.equal(got, b.run())
 
 
+@pytest.mark.parametrize("fmt,dtype", [("int8", torch.float32), ("e4m3", torch.bfloat16)])
+@pytest.mark.parametrize("req,queries,rows,heads", [(90, 1, 9000, "0.5b"), (2, 1000, 7000, "0.5b"), (24, 5, 9000, "14b")])
+def test_attend_more_work_than_units(req, queries, rows, heads, fmt, dtype):
+    """Two shares to a unit, of different lengths, for each tiling; pages that requests share."""
+    H_q, H, d = HEADS[heads]
+    rng = np.random.default_rng(req)
+    b = Batch(req, [2000], [1], HEADS[heads], 16, fmt)
+    b.lens, b.counts = rng.integers(rows // 2, rows, req), np.full(req, queries)
+    b.table = rng.integers(0, b.pages.n_pages, (req, -(-rows // 16)))
+    b.starts = np.arange(req + 1) * queries
+    b.q = bf16(rng.standard_normal((req * queries, H_q, d)))
+    got = b.run(True, dtype)
+    b.check(got, b.want(True))
+    assert torch.equal(got, b.run(True, dtype))
+
+
 def test_attend_thousands_of_short_requests():
     """Too many for every workgroup of a whole tile to read them: shares of many tiles each."""
     rng = np.random.default_rng(8)
