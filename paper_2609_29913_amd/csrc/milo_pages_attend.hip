@@ -15,7 +15,7 @@
 //  - many columns: the vector units and the matrix units together, which hardly
 //    overlap here (2048 queries, the last of 8192 rows, 7B heads, E4M3: 232 us, 905
 //    TFLOP/s, where a matrix product of 16384^3 reaches 1328; the matrix units are busy
-//    37% of the cycles, the vector units issue in 63% of them).  Half of the vector
+//    39% of the cycles, the vector units issue in 69% of them).  Half of the vector
 //    instructions are the codes' conversions, which INT8 needs more of (about 300 us).
 //  - in between (32 columns): the longest tile (8 requests of 100 .. 3000 rows, 1 .. 37
 //    queries that see all of them, 14B heads: 27 us; the first tiles end after 9).
